@@ -1,0 +1,75 @@
+/*
+ * mux_pref.h -- C ABI of the preference loss of pairs of sequences of a chunk-aligned batch.
+ *
+ * A task that learns from preferences brings pairs of sequences, an answer that was chosen and one that was rejected.
+ * With lp_i the log-probability of row i's label under the logits of that row and L_s the sum of lp_i over the counted rows
+ * of sequence s, a pair (c, r) with the reference's sums R costs
+ *     m = beta ((L_c - R_c) - (L_r - R_r)) ,   loss = -(1 - e) log sigma(m) - e log sigma(-m)        (paired log ratios)
+ * with sigma(z) = 1 / (1 + exp(-z)) and e the pair's label smoothing.  Backward, with the pairs' weights dloss,
+ *     c_s = sum over the pairs with chosen = s of  dloss dloss/dm beta  -  the same over those with rejected = s
+ *     dlogits_i = c_s (onehot(label_i) - softmax(logits_i))                   (row i counted, of sequence s)
+ * The reference is usually the same backbone with the adapters off: a forward without pairs over its logits gives R.
+ *
+ * Sequences are numbered as in the table's serialisation (task by task, each in the order of its seq_lens).  A row is counted
+ * if it holds a token and its label lies in 0 .. vocab - 1; labels are those of the row itself (the caller has shifted
+ * them), and any other value (-1, -100) leaves the row out: a prompt's rows, a sequence's last.  A sequence may be in any number of
+ * pairs and on either side of them; both sequences of a pair belong to one task.
+ *
+ * Conventions as in mux.h.  logits, dlogits: device [T, vocab], bf16 or fp32, with leading dimensions >= vocab and pointers
+ * aligned to their element; dlogits may be the logits' own memory (same pointer, same leading dimension).  labels: device
+ * int32 [T].  ref_logp, logp: device fp32 [number of sequences]; row_logp: device fp32 [T]; loss, dloss: device fp32
+ * [n_pairs].  The content of rows that are not counted is never read.  Row maxima and sums over the vocabulary are fp32, sums over
+ * a sequence's rows, margins and losses 64-bit until they are stored.  Infinite and NaN logits give what the formulas give.
+ */
+#ifndef MUX_PREF_H_
+#define MUX_PREF_H_
+
+#include <stddef.h>
+#include <stdint.h>
+
+#include "mux.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+typedef struct {
+  int32_t chosen, rejected; /* sequence numbers, two different sequences of one task               */
+  float beta;               /* > 0, finite                                                         */
+  float smoothing;          /* e, 0 .. 1                                                           */
+} mux_pref_pair;
+
+typedef struct {
+  int32_t vocab;            /* >= 1                                                                */
+  int32_t dtype;            /* mux_dtype of logits and dlogits                                     */
+  int64_t ld, ldg;          /* elements between rows of the logits and of dlogits, >= vocab        */
+} mux_pref_desc;
+
+/* Lays the pairs out for the calls below: which sequence a row belongs to, which pairs a sequence is in.  pairs: host
+ * array of n_pairs (may be 0: log-probabilities only); host_dst: mux_pref_layout_bytes() bytes of the caller, who copies
+ * them to the device (4-byte aligned).  Index work on the host; nothing is launched.  The calls take the table and the number of
+ * pairs that the layout was made with. */
+size_t mux_pref_layout_bytes(const mux_segtab* st, int32_t n_pairs);
+mux_status mux_pref_layout(const mux_segtab* st, const mux_pref_pair* pairs, int32_t n_pairs, void* host_dst, size_t cap);
+
+/* Bytes of `saved` (forward -> backward: maximum and reciprocal sum of every counted row, slope of every pair) and of the
+ * forward's workspace (both 8-byte aligned).  Host arithmetic. */
+size_t mux_pref_saved_bytes(const mux_pref_desc* desc, const mux_segtab* st, int32_t n_pairs);
+size_t mux_pref_workspace_bytes(const mux_pref_desc* desc, const mux_segtab* st);
+
+/* Forward.  row_logp (zero where a row is not counted) and logp (zero for a sequence without counted rows) may be NULL;
+ * `saved` may be NULL when no backward pass follows.  With n_pairs = 0, ref_logp and loss are not read or written (NULL). */
+mux_status mux_pref_forward(const mux_pref_desc* desc, const mux_segtab* st, const void* dev_layout, int32_t n_pairs,
+                            const void* logits, const int32_t* labels, const float* ref_logp, float* row_logp, float* logp,
+                            float* loss, void* saved, void* ws, size_t ws_bytes, void* hip_stream);
+
+/* Backward: every row of dlogits is written, with zero where it is not counted or its sequence is in no pair.  `saved` is the
+ * forward's, logits and labels what it was given. */
+mux_status mux_pref_backward(const mux_pref_desc* desc, const mux_segtab* st, const void* dev_layout, int32_t n_pairs,
+                             const void* logits, const int32_t* labels, const void* saved, const float* dloss, void* dlogits,
+                             void* hip_stream);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* MUX_PREF_H_ */

@@ -24,6 +24,9 @@ __all__ = [
     "CostModel", "mux_plan_stage_latency", "mux_plan_htask_latency", "mux_plan_fusion",
     "mux_dispatch_gather", "mux_dispatch_scatter",
     "AttnDesc", "mux_attn_saved_bytes", "mux_attn_workspace_bytes", "mux_attn_forward", "mux_attn_backward",
+    "NormDesc", "MUX_NORM_MAX_WIDTH", "mux_norm_saved_bytes", "mux_norm_workspace_bytes", "mux_norm_forward", "mux_norm_backward",
+    "PrefDesc", "mux_pref_layout_bytes", "mux_pref_layout", "mux_pref_saved_bytes", "mux_pref_workspace_bytes",
+    "mux_pref_forward", "mux_pref_backward",
     "mux_probe_mfma_operand_bytes", "mux_probe_mfma_sink_bytes", "mux_probe_mfma",
     "mux_probe_read_sink_bytes", "mux_probe_read", "mux_diag_set_clock_buffer",
 ]
@@ -35,6 +38,7 @@ MUX_SEGTAB_DENSE = 1
 MUX_LAYER_REFERENCE_KERNELS = 1
 MUX_MAX_RANK = 64
 MUX_STATIC_WS_BYTES = 32 << 20
+MUX_NORM_MAX_WIDTH = 32768
 
 _STATUS_NAMES = {1: "MUX_ERR_INVALID_ARG", 2: "MUX_ERR_SHAPE", 3: "MUX_ERR_UNSUPPORTED", 4: "MUX_ERR_WORKSPACE",
                  5: "MUX_ERR_HOST_NOMEM", 6: "MUX_ERR_DEVICE"}
@@ -79,6 +83,26 @@ class AttnDesc:
                  n_kv_heads: Optional[int] = None, dtype: int = MUX_DT_BF16):
         self.c = _AttnDescC(int(n_heads), int(n_heads if n_kv_heads is None else n_kv_heads), int(head_dim), int(dtype),
                             float(scale), int(ldq), int(ldk), int(ldv), int(ldo))
+
+
+class _NormDescC(ctypes.Structure):
+    _fields_ = [("width", c_int32), ("dtype", c_int32), ("eps", c_float), ("ldx", c_int64), ("ldy", c_int64),
+                ("n_tasks", c_int32), ("gamma", POINTER(c_void_p)), ("beta", POINTER(c_void_p))]
+
+
+class _PrefPairC(ctypes.Structure):
+    _fields_ = [("chosen", c_int32), ("rejected", c_int32), ("beta", c_float), ("smoothing", c_float)]
+
+
+class _PrefDescC(ctypes.Structure):
+    _fields_ = [("vocab", c_int32), ("dtype", c_int32), ("ld", c_int64), ("ldg", c_int64)]
+
+
+class PrefDesc:
+    """mux_pref_desc (include/mux_pref.h); leading dimensions default to the vocabulary."""
+
+    def __init__(self, vocab: int, dtype: int = MUX_DT_BF16, ld: Optional[int] = None, ldg: Optional[int] = None):
+        self.c = _PrefDescC(int(vocab), int(dtype), int(vocab if ld is None else ld), int(vocab if ldg is None else ldg))
 
 
 class _CurveC(ctypes.Structure):
@@ -188,6 +212,16 @@ def load_library() -> ctypes.CDLL:
         "mux_attn_workspace_bytes": (c_size_t, [POINTER(_AttnDescC), vp]),
         "mux_attn_forward": (c_int, [POINTER(_AttnDescC), vp, vp, vp, vp, vp, vp, vp, vp]),
         "mux_attn_backward": (c_int, [POINTER(_AttnDescC), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, c_size_t, vp]),
+        "mux_norm_saved_bytes": (c_size_t, [POINTER(_NormDescC), vp]),
+        "mux_norm_workspace_bytes": (c_size_t, [POINTER(_NormDescC), vp]),
+        "mux_norm_forward": (c_int, [POINTER(_NormDescC), vp, vp, vp, vp, vp, vp]),
+        "mux_norm_backward": (c_int, [POINTER(_NormDescC), vp, vp, vp, vp, vp, vp, POINTER(vp), POINTER(vp), c_int, vp, c_size_t, vp]),
+        "mux_pref_layout_bytes": (c_size_t, [vp, c_int32]),
+        "mux_pref_layout": (c_int, [vp, POINTER(_PrefPairC), c_int32, vp, c_size_t]),
+        "mux_pref_saved_bytes": (c_size_t, [POINTER(_PrefDescC), vp, c_int32]),
+        "mux_pref_workspace_bytes": (c_size_t, [POINTER(_PrefDescC), vp]),
+        "mux_pref_forward": (c_int, [POINTER(_PrefDescC), vp, vp, c_int32, vp, vp, vp, vp, vp, vp, vp, vp, c_size_t, vp]),
+        "mux_pref_backward": (c_int, [POINTER(_PrefDescC), vp, vp, c_int32, vp, vp, vp, vp, vp, vp]),
         "mux_plan_stage_latency": (c_int, [POINTER(_CostModelC), c_int32, c_int32, POINTER(c_int64), POINTER(ctypes.c_double)]),
         "mux_plan_htask_latency": (c_int, [POINTER(_CostModelC), c_int32, POINTER(c_int64), POINTER(ctypes.c_double)]),
         "mux_plan_fusion": (c_int, [POINTER(_CostModelC), c_int32, POINTER(c_int64), c_int32, POINTER(c_int32),
@@ -324,6 +358,22 @@ class LayerDesc:
                              L=ctypes.cast(self._L, POINTER(c_void_p)),
                              masks=ctypes.cast(self._masks, POINTER(POINTER(_SparseMaskC))) if masks is not None else None)
         self.n_tasks = int(n_tasks)
+
+
+class NormDesc:
+    """mux_norm_desc (include/mux_norm.h); gamma and beta: one device tensor (or None) per task, `n_tasks` where both lists are
+    None.  Keeps the pointer arrays alive; leading dimensions default to the width."""
+
+    def __init__(self, width: int, dtype: int, gamma=None, beta=None, eps: float = 1e-5, ldx: Optional[int] = None,
+                 ldy: Optional[int] = None, n_tasks: Optional[int] = None):
+        if n_tasks is None:
+            n_tasks = len(gamma if gamma is not None else beta)
+        self.n_tasks = int(n_tasks)
+        self._gamma, self._beta = _ptr_array(gamma, self.n_tasks), _ptr_array(beta, self.n_tasks)
+        self._keep = (gamma, beta)
+        self.c = _NormDescC(width=int(width), dtype=int(dtype), eps=float(eps), ldx=int(width if ldx is None else ldx),
+                            ldy=int(width if ldy is None else ldy), n_tasks=self.n_tasks,
+                            gamma=ctypes.cast(self._gamma, POINTER(c_void_p)), beta=ctypes.cast(self._beta, POINTER(c_void_p)))
 
 
 # ------------------------------------------------------------------ same names as the header
@@ -529,6 +579,64 @@ def mux_attn_backward(desc: AttnDesc, st: SegTab, dev_segtab, Q, K, V, O, dO, sa
     _check(load_library().mux_attn_backward(ctypes.byref(desc.c), st.handle, _ptr(dev_segtab), _ptr(Q), _ptr(K), _ptr(V),
                                             _ptr(O), _ptr(dO), _ptr(saved), _ptr(dQ), _ptr(dK), _ptr(dV), _ptr(ws),
                                             int(ws_bytes), _stream(stream)))
+
+
+def mux_norm_saved_bytes(desc: NormDesc, st: SegTab) -> int:
+    return int(load_library().mux_norm_saved_bytes(ctypes.byref(desc.c), st.handle))
+
+
+def mux_norm_workspace_bytes(desc: NormDesc, st: SegTab) -> int:
+    return int(load_library().mux_norm_workspace_bytes(ctypes.byref(desc.c), st.handle))
+
+
+def mux_norm_forward(desc: NormDesc, st: SegTab, dev_segtab, X, Y, saved, stream=None) -> None:
+    _check(load_library().mux_norm_forward(ctypes.byref(desc.c), st.handle, _ptr(dev_segtab), _ptr(X), _ptr(Y), _ptr(saved),
+                                           _stream(stream)))
+
+
+def mux_norm_backward(desc: NormDesc, st: SegTab, dev_segtab, X, dY, saved, dX, dgamma, dbeta, accumulate: int, ws,
+                      ws_bytes: int, stream=None) -> None:
+    pg, pb = _ptr_array(dgamma, desc.n_tasks), _ptr_array(dbeta, desc.n_tasks)
+    _check(load_library().mux_norm_backward(
+        ctypes.byref(desc.c), st.handle, _ptr(dev_segtab), _ptr(X), _ptr(dY), _ptr(saved), _ptr(dX),
+        ctypes.cast(pg, POINTER(c_void_p)), ctypes.cast(pb, POINTER(c_void_p)), int(accumulate), _ptr(ws), int(ws_bytes),
+        _stream(stream)))
+
+
+def mux_pref_layout_bytes(st: SegTab, n_pairs: int) -> int:
+    return int(load_library().mux_pref_layout_bytes(st.handle, int(n_pairs)))
+
+
+def mux_pref_layout(st: SegTab, pairs: Sequence) -> np.ndarray:
+    """The layout of the pairs (chosen, rejected, beta, smoothing) as a host array of int32, to be copied to the device."""
+    arr = (_PrefPairC * max(len(pairs), 1))()
+    for i, (c, r, beta, smoothing) in enumerate(pairs):
+        arr[i] = _PrefPairC(int(c), int(r), float(beta), float(smoothing))
+    n = mux_pref_layout_bytes(st, len(pairs))
+    out = np.zeros(n // 4, dtype=np.int32)
+    _check(load_library().mux_pref_layout(st.handle, arr, len(pairs), out.ctypes.data, n))
+    return out
+
+
+def mux_pref_saved_bytes(desc: PrefDesc, st: SegTab, n_pairs: int) -> int:
+    return int(load_library().mux_pref_saved_bytes(ctypes.byref(desc.c), st.handle, int(n_pairs)))
+
+
+def mux_pref_workspace_bytes(desc: PrefDesc, st: SegTab) -> int:
+    return int(load_library().mux_pref_workspace_bytes(ctypes.byref(desc.c), st.handle))
+
+
+def mux_pref_forward(desc: PrefDesc, st: SegTab, dev_layout, n_pairs: int, logits, labels, ref_logp, row_logp, logp, loss,
+                     saved, ws, ws_bytes: int, stream=None) -> None:
+    _check(load_library().mux_pref_forward(ctypes.byref(desc.c), st.handle, _ptr(dev_layout), int(n_pairs), _ptr(logits),
+                                           _ptr(labels), _ptr(ref_logp), _ptr(row_logp), _ptr(logp), _ptr(loss), _ptr(saved),
+                                           _ptr(ws), int(ws_bytes), _stream(stream)))
+
+
+def mux_pref_backward(desc: PrefDesc, st: SegTab, dev_layout, n_pairs: int, logits, labels, saved, dloss, dlogits,
+                      stream=None) -> None:
+    _check(load_library().mux_pref_backward(ctypes.byref(desc.c), st.handle, _ptr(dev_layout), int(n_pairs), _ptr(logits),
+                                            _ptr(labels), _ptr(saved), _ptr(dloss), _ptr(dlogits), _stream(stream)))
 
 
 def mux_dispatch_gather(st: SegTab, dev_segtab, task_ptrs: Sequence, ld_task: int, aligned, ld_aligned: int, width: int,

@@ -1,0 +1,461 @@
+// Preference loss of pairs of sequences from the logits of the batch (mux_pref.h), forward and backward.
+//
+// The logits are all there is to move: the forward reads them once, the backward reads them once and writes as much; what is
+// computed from them is one exponential an element.  A workgroup takes a slab of a row's vocabulary, so that a few rows fill the chip as
+// well as many do, and holds it in registers: maximum, then the sum of exponentials against it, one read.  The slabs' (maximum, sum)
+// pairs are joined by the launch that sums the rows of each sequence, a fixed number of terms in a fixed order; a third launch
+// forms the pairs' losses and slopes.  Rows that are not counted are never read.
+// Rows may begin anywhere (a vocabulary of odd size): what lies before a row's first 16-byte boundary and behind its last
+// belongs to the first and the last slab, element by element; the rest moves in 16-byte pieces.
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <new>
+#include <vector>
+
+#include "mux_device_utils.h"
+#include "mux_pref.h"
+
+namespace mux {
+namespace {
+
+// device image of mux_pref_layout: a header of int32 words, then the sections whose word offsets it gives
+enum : int {
+  PH_MAGIC = 0, PH_T, PH_NSEQS, PH_NPAIRS,
+  PH_OFF_ROW_SEQ,          // [T] sequence of the row, -1: padding
+  PH_OFF_SEQ,              // [n_seqs] first row, length
+  PH_OFF_PAIR,             // [n_pairs] mux_pref_pair
+  PH_OFF_PTR, PH_OFF_ENT,  // the pairs of sequence s: entries ptr[s] .. ptr[s + 1] - 1, each 2 * pair + (1: rejected)
+  PH_WORDS = 16
+};
+constexpr int32_t kPrefMagic = 0x5250554D;
+constexpr int kThreads = 256;
+constexpr int kPieces = 4;                         // 16-byte pieces a thread holds of a slab
+constexpr float LOG2E = 1.4426950408889634f;
+
+template <class S> constexpr int per_piece() { return 16 / (int)sizeof(S); }
+
+struct PrefParams {
+  const int32_t* layout;
+  const void* logits;
+  void* dlogits;
+  const int32_t* labels;
+  const float *ref, *dloss;
+  float *row_logp, *logp, *loss;
+  float2* part;            // forward: [T][slabs] (maximum, sum of exp(x - maximum))
+  double* seq_logp;        // forward: [n_seqs]
+  float2* stat;            // saved: [T] (maximum, 1 / sum), null: not kept
+  float* slope;            // saved: [n_pairs]
+  int64_t ld, ldg;
+  int T, V, n_seqs, n_pairs, slabs, slab;          // slab: elements, a multiple of a piece
+};
+
+__device__ __forceinline__ float elem(const uint4& r, int i, bf16_t) {
+  const uint32_t w = i < 2 ? r.x : i < 4 ? r.y : i < 6 ? r.z : r.w;
+  return __uint_as_float(i & 1 ? w & 0xffff0000u : w << 16);
+}
+__device__ __forceinline__ float elem(const uint4& r, int i, float) {
+  return __uint_as_float(i == 0 ? r.x : i == 1 ? r.y : i == 2 ? r.z : r.w);
+}
+__device__ __forceinline__ float fast_exp(float x) { return __builtin_amdgcn_exp2f(x * LOG2E); }
+
+// A workgroup's share of a row: pieces [first, first + n) of E elements from the row's first 16-byte boundary on, and the loose
+// elements before it (first slab) and behind the last piece (last slab).
+template <class S>
+struct Slab {
+  static constexpr int E = per_piece<S>();
+  int head, first, n, tail0, tails;
+  __device__ __forceinline__ Slab(const S* row, int V, int slab_elems, int k, int slabs) {
+    const int h = min((int)((16 - ((uintptr_t)row & 15)) & 15) / (int)sizeof(S), V);
+    const int all = (V - h) / E, per = slab_elems / E;
+    head = k == 0 ? h : 0;
+    first = min(k * per, all);
+    n = min(per, all - first);
+    first = h + first * E;                                     // as an element of the row
+    tail0 = h + all * E;
+    tails = k == slabs - 1 ? V - tail0 : 0;
+  }
+};
+
+__device__ __forceinline__ bool counted(const PrefParams& p, int row, int& seq, int& label) {
+  seq = p.layout[p.layout[PH_OFF_ROW_SEQ] + row];
+  label = p.labels[row];
+  return seq >= 0 && label >= 0 && label < p.V;
+}
+
+// (maximum, sum) of two parts of a row
+__device__ __forceinline__ void join(float& m, float& s, float m2, float s2) {
+  const float top = fmaxf(m, m2), ref = top == -INFINITY ? 0.f : top;
+  s = s * fast_exp(m - ref) + s2 * fast_exp(m2 - ref);
+  m = top;
+}
+
+template <class S>
+__global__ __launch_bounds__(kThreads) void k_pref_rows(PrefParams p) {
+  constexpr int E = per_piece<S>();
+  __shared__ float lds[2][kThreads / 64];
+  const int row = (int)(blockIdx.x / (unsigned)p.slabs), k = (int)(blockIdx.x % (unsigned)p.slabs);
+  int seq, label;
+  if (!counted(p, row, seq, label)) return;
+  const S* x = (const S*)p.logits + (size_t)row * p.ld;
+  const Slab<S> sl(x, p.V, p.slab, k, p.slabs);
+  const int tid = threadIdx.x;
+  uint4 none;                                                    // pieces of -inf
+  none.x = none.y = none.z = none.w = sizeof(S) == 2 ? 0xFF80FF80u : 0xFF800000u;
+  uint4 v[kPieces];
+#pragma unroll
+  for (int i = 0; i < kPieces; ++i) {
+    const int e = tid + i * kThreads;
+    v[i] = e < sl.n ? *(const uint4*)(x + sl.first + (size_t)e * E) : none;
+  }
+  float loose = -INFINITY;                                       // (one of at most 2 E - 2 elements outside the pieces)
+  if (tid < sl.head) loose = Store<S>::ld(x, tid);
+  else if (tid >= 64 && tid - 64 < sl.tails) loose = Store<S>::ld(x, sl.tail0 + tid - 64);
+  float m = loose;
+#pragma unroll
+  for (int i = 0; i < kPieces; ++i)
+#pragma unroll
+    for (int e = 0; e < E; ++e) m = fmaxf(m, elem(v[i], e, S()));
+  const float ref = m == -INFINITY ? 0.f : m;
+  float s = fast_exp(loose - ref);
+#pragma unroll
+  for (int i = 0; i < kPieces; ++i)
+#pragma unroll
+    for (int e = 0; e < E; ++e) s += fast_exp(elem(v[i], e, S()) - ref);
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) join(m, s, __shfl_xor(m, o), __shfl_xor(s, o));
+  if ((tid & 63) == 0) { lds[0][tid >> 6] = m; lds[1][tid >> 6] = s; }
+  __syncthreads();
+  if (tid == 0) {
+#pragma unroll
+    for (int w = 1; w < kThreads / 64; ++w) join(m, s, lds[0][w], lds[1][w]);
+    p.part[(size_t)row * p.slabs + k] = float2{m, s};
+  }
+}
+
+// One workgroup a sequence: joins the slabs of its rows and sums the rows' log-probabilities.  Workgroups from n_seqs on
+// clear row_logp of the rows that belong to no sequence.
+template <class S>
+__global__ __launch_bounds__(1024) void k_pref_seqs(PrefParams p) {
+  __shared__ double lds[16];
+  const int tid = threadIdx.x;
+  if ((int)blockIdx.x >= p.n_seqs) {
+    const int row = ((int)blockIdx.x - p.n_seqs) * 1024 + tid;
+    if (row < p.T && p.layout[p.layout[PH_OFF_ROW_SEQ] + row] < 0) p.row_logp[row] = 0.f;
+    return;
+  }
+  const int32_t* q = p.layout + p.layout[PH_OFF_SEQ] + 2 * (int)blockIdx.x;
+  const int first = q[0], len = q[1];
+  double sum = 0.0;
+  for (int r = tid; r < len; r += 1024) {
+    const int row = first + r, label = p.labels[row];
+    double lp = 0.0;
+    if (label >= 0 && label < p.V) {
+      const float x = Store<S>::ld((const S*)p.logits, (size_t)row * p.ld + label);
+      float2 a = p.part[(size_t)row * p.slabs];
+      for (int k = 1; k < p.slabs; ++k) {
+        const float2 b = p.part[(size_t)row * p.slabs + k];
+        join(a.x, a.y, b.x, b.y);
+      }
+      lp = (double)(x - a.x) - log((double)a.y);
+      if (p.stat) p.stat[row] = float2{a.x, 1.f / a.y};
+    }
+    if (p.row_logp) p.row_logp[row] = (float)lp;
+    sum += lp;
+  }
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) sum += __shfl_xor(sum, o);
+  if ((tid & 63) == 0) lds[tid >> 6] = sum;
+  __syncthreads();
+  if (tid == 0) {
+    sum = 0.0;
+    for (int w = 0; w < 16; ++w) sum += lds[w];
+    p.seq_logp[blockIdx.x] = sum;
+    if (p.logp) p.logp[blockIdx.x] = (float)sum;
+  }
+}
+
+__device__ __forceinline__ double softplus(double z) { return fmax(z, 0.0) + log1p(exp(-fabs(z))); }
+__device__ __forceinline__ double sigmoid(double z) { return 1.0 / (1.0 + exp(-z)); }
+
+__global__ __launch_bounds__(256) void k_pref_pairs(PrefParams p) {
+  const int i = (int)blockIdx.x * 256 + (int)threadIdx.x;
+  if (i >= p.n_pairs) return;
+  const int32_t* q = p.layout + p.layout[PH_OFF_PAIR] + 4 * i;
+  const int c = q[0], r = q[1];
+  const double beta = __int_as_float(q[2]), e = __int_as_float(q[3]);
+  const double m = beta * ((p.seq_logp[c] - (double)p.ref[c]) - (p.seq_logp[r] - (double)p.ref[r]));
+  // (a term whose weight is zero is left out: it may be infinite)
+  double loss = 0.0, slope = 0.0;
+  if (e < 1.0) { loss += (1.0 - e) * softplus(-m); slope -= (1.0 - e) * sigmoid(-m); }
+  if (e > 0.0) { loss += e * softplus(m); slope += e * sigmoid(m); }
+  p.loss[i] = (float)loss;
+  if (p.slope) p.slope[i] = (float)(beta * slope);
+}
+
+template <class S>
+__device__ __forceinline__ uint4 pack(const float* v);
+template <>
+__device__ __forceinline__ uint4 pack<bf16_t>(const float* v) {
+  return uint4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+}
+template <>
+__device__ __forceinline__ uint4 pack<float>(const float* v) {
+  return uint4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+}
+
+// grid = (row, slab) as in k_pref_rows.  SAME: every row of dlogits begins at the same place inside 16 bytes as that of the logits.
+template <class S, bool SAME>
+__global__ __launch_bounds__(kThreads) void k_pref_bwd(PrefParams p) {
+  constexpr int E = per_piece<S>();
+  const int row = (int)(blockIdx.x / (unsigned)p.slabs), k = (int)(blockIdx.x % (unsigned)p.slabs);
+  const int tid = threadIdx.x;
+  int seq, label;
+  const bool on = counted(p, row, seq, label);
+  const S* x = (const S*)p.logits + (size_t)row * p.ld;
+  S* d = (S*)p.dlogits + (size_t)row * p.ldg;
+  int e0 = 0, e1 = 0;
+  if (on) {
+    const int32_t* ptr = p.layout + p.layout[PH_OFF_PTR] + seq;
+    e0 = ptr[0]; e1 = ptr[1];
+  }
+  if (e0 == e1) {                                                // not counted, or in no pair: zero, whatever the logits hold
+    const Slab<S> sl(d, p.V, p.slab, k, p.slabs);
+    for (int e = tid; e < sl.n; e += kThreads) *(uint4*)(d + sl.first + (size_t)e * E) = uint4{0u, 0u, 0u, 0u};
+    if (tid < sl.head) d[tid] = S(0);
+    else if (tid >= 64 && tid - 64 < sl.tails) d[sl.tail0 + tid - 64] = S(0);
+    return;
+  }
+  const Slab<S> sl(x, p.V, p.slab, k, p.slabs);
+  uint4 v[kPieces];
+#pragma unroll
+  for (int i = 0; i < kPieces; ++i) {
+    const int e = tid + i * kThreads;
+    v[i] = uint4{0u, 0u, 0u, 0u};
+    if (e < sl.n) v[i] = *(const uint4*)(x + sl.first + (size_t)e * E);
+  }
+  double cs = 0.0;                                               // (the same sum in every thread)
+  for (int i = e0; i < e1; ++i) {
+    const int ent = p.layout[p.layout[PH_OFF_ENT] + i], pair = ent >> 1;
+    const double w = (double)p.dloss[pair] * (double)p.slope[pair];
+    cs += ent & 1 ? -w : w;
+  }
+  const float c = (float)cs;
+  const float2 st = p.stat[row];
+  const float f = -c * st.y;
+#pragma unroll
+  for (int i = 0; i < kPieces; ++i) {
+    const int e = tid + i * kThreads;
+    if (e >= sl.n) continue;
+    float o[E];
+    const int at = sl.first + e * E;
+#pragma unroll
+    for (int j = 0; j < E; ++j) {
+      o[j] = f * fast_exp(elem(v[i], j, S()) - st.x);
+      if (at + j == label) o[j] += c;
+    }
+    if constexpr (SAME) *(uint4*)(d + at) = pack<S>(o);
+    else
+#pragma unroll
+      for (int j = 0; j < E; ++j) Store<S>::st(d, (size_t)at + j, o[j]);
+  }
+  int at = -1;
+  if (tid < sl.head) at = tid;
+  else if (tid >= 64 && tid - 64 < sl.tails) at = sl.tail0 + tid - 64;
+  if (at >= 0) Store<S>::st(d, (size_t)at, f * fast_exp(Store<S>::ld(x, (size_t)at) - st.x) + (at == label ? c : 0.f));
+}
+
+int n_seqs(const mux_segtab* st) { return st->image[11]; }
+const int32_t* seq_words(const mux_segtab* st) {               // [task, pack, first_row, len] of every sequence
+  return st->image.data() + 16 + 8 * (size_t)st->image[3] + 6 * (size_t)st->image[9] + 4 * (size_t)st->image[6] + 6 * (size_t)st->image[10];
+}
+
+size_t esize(const mux_pref_desc* d) { return d->dtype == MUX_DT_F32 ? 4 : 2; }
+
+// A row's slabs: as few as its elements need, of nearly the same size.
+void cut(const mux_pref_desc* d, int& slabs, int& slab) {
+  const int e = 16 / (int)esize(d), most = kThreads * kPieces * e;
+  slabs = (int)(((int64_t)d->vocab + most - 1) / most);
+  slab = (int)((((int64_t)d->vocab + slabs - 1) / slabs + e - 1) / e * e);
+}
+
+mux_status check(const char* fn, const mux_pref_desc* d, const mux_segtab* st, int32_t n_pairs, bool grad) {
+  if (!d || !st) return fail(MUX_ERR_INVALID_ARG, std::string(fn) + ": null descriptor or table");
+  if (d->dtype != MUX_DT_BF16 && d->dtype != MUX_DT_F32) return fail(MUX_ERR_INVALID_ARG, std::string(fn) + ": unknown dtype");
+  if (d->vocab < 1 || n_pairs < 0) return fail(MUX_ERR_INVALID_ARG, std::string(fn) + ": vocab must be positive, n_pairs not negative");
+  if (d->vocab > (1 << 30)) return fail(MUX_ERR_SHAPE, std::string(fn) + ": problem too large");
+  const int64_t ld = grad ? std::max(d->ld, d->ldg) : d->ld;
+  if (d->ld < d->vocab || (grad && d->ldg < d->vocab)) return fail(MUX_ERR_SHAPE, std::string(fn) + ": a leading dimension is smaller than the vocabulary");
+  int slabs, slab;
+  cut(d, slabs, slab);
+  if (ld >= ((int64_t)1 << 40) || (int64_t)st->T * ld >= ((int64_t)1 << 42) || (int64_t)st->T * slabs >= ((int64_t)1 << 31) ||
+      n_pairs > (1 << 28))
+    return fail(MUX_ERR_SHAPE, std::string(fn) + ": problem too large");
+  return MUX_OK;
+}
+
+size_t extent(const mux_pref_desc* d, const mux_segtab* st, int64_t ld) {
+  return st->T > 0 ? ((size_t)(st->T - 1) * (size_t)ld + (size_t)d->vocab) * esize(d) : 0;
+}
+
+struct Bytes { const void* p; size_t n; };
+
+mux_status last_hip(const char* fn) {
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return fail(MUX_ERR_DEVICE, std::string(fn) + ": " + hipGetErrorString(e));
+  return MUX_OK;
+}
+
+}  // namespace
+}  // namespace mux
+
+using namespace mux;
+
+extern "C" size_t mux_pref_layout_bytes(const mux_segtab* st, int32_t n_pairs) {
+  if (!st || n_pairs < 0) return 0;
+  const size_t s = (size_t)n_seqs(st);
+  return (PH_WORDS + (size_t)st->T + 2 * s + 4 * (size_t)n_pairs + s + 1 + 2 * (size_t)n_pairs) * 4;
+}
+
+extern "C" mux_status mux_pref_layout(const mux_segtab* st, const mux_pref_pair* pairs, int32_t n_pairs, void* host_dst, size_t cap) {
+  static const char* fn = "mux_pref_layout";
+  static_assert(sizeof(mux_pref_pair) == 16, "four words a pair");
+  if (!st || n_pairs < 0 || (n_pairs > 0 && !pairs) || !host_dst) return fail(MUX_ERR_INVALID_ARG, std::string(fn) + ": null argument or negative n_pairs");
+  if (n_pairs > (1 << 28)) return fail(MUX_ERR_SHAPE, std::string(fn) + ": problem too large");
+  if (cap < mux_pref_layout_bytes(st, n_pairs)) return fail(MUX_ERR_WORKSPACE, std::string(fn) + ": destination too small");
+  const int S = n_seqs(st);
+  const int32_t* seq = seq_words(st);
+  for (int32_t i = 0; i < n_pairs; ++i) {
+    const mux_pref_pair& q = pairs[i];
+    if (q.chosen < 0 || q.chosen >= S || q.rejected < 0 || q.rejected >= S) return fail(MUX_ERR_SHAPE, std::string(fn) + ": no such sequence");
+    if (q.chosen == q.rejected) return fail(MUX_ERR_INVALID_ARG, std::string(fn) + ": a pair of one sequence");
+    if (seq[4 * q.chosen] != seq[4 * q.rejected]) return fail(MUX_ERR_INVALID_ARG, std::string(fn) + ": a pair of sequences of two tasks");
+    if (!(q.beta > 0.f) || !(q.beta < INFINITY) || !(q.smoothing >= 0.f) || !(q.smoothing <= 1.f))
+      return fail(MUX_ERR_INVALID_ARG, std::string(fn) + ": beta must be positive and finite, smoothing in 0 .. 1");
+  }
+  int32_t* w = (int32_t*)host_dst;
+  std::memset(w, 0, PH_WORDS * 4);
+  w[PH_MAGIC] = kPrefMagic; w[PH_T] = st->T; w[PH_NSEQS] = S; w[PH_NPAIRS] = n_pairs;
+  int32_t at = PH_WORDS;
+  w[PH_OFF_ROW_SEQ] = at; at += st->T;
+  w[PH_OFF_SEQ] = at; at += 2 * S;
+  w[PH_OFF_PAIR] = at; at += 4 * n_pairs;
+  w[PH_OFF_PTR] = at; at += S + 1;
+  w[PH_OFF_ENT] = at;
+  int32_t *row_seq = w + w[PH_OFF_ROW_SEQ], *ptr = w + w[PH_OFF_PTR], *ent = w + w[PH_OFF_ENT];
+  for (int32_t i = 0; i < st->T; ++i) row_seq[i] = -1;
+  for (int32_t s = 0; s < S; ++s) {
+    const int32_t first = seq[4 * s + 2], len = seq[4 * s + 3];
+    w[w[PH_OFF_SEQ] + 2 * s] = first;
+    w[w[PH_OFF_SEQ] + 2 * s + 1] = len;
+    for (int32_t r = 0; r < len; ++r) row_seq[first + r] = s;
+  }
+  if (n_pairs > 0) std::memcpy(w + w[PH_OFF_PAIR], pairs, (size_t)n_pairs * sizeof(mux_pref_pair));
+  for (int32_t s = 0; s <= S; ++s) ptr[s] = 0;
+  for (int32_t i = 0; i < n_pairs; ++i) { ptr[pairs[i].chosen + 1]++; ptr[pairs[i].rejected + 1]++; }
+  for (int32_t s = 0; s < S; ++s) ptr[s + 1] += ptr[s];
+  try {
+    std::vector<int32_t> next(ptr, ptr + S);
+    for (int32_t i = 0; i < n_pairs; ++i) { ent[next[pairs[i].chosen]++] = 2 * i; ent[next[pairs[i].rejected]++] = 2 * i + 1; }
+  } catch (const std::bad_alloc&) {
+    return fail(MUX_ERR_HOST_NOMEM, std::string(fn) + ": out of host memory");
+  }
+  return MUX_OK;
+}
+
+extern "C" size_t mux_pref_saved_bytes(const mux_pref_desc* desc, const mux_segtab* st, int32_t n_pairs) {
+  if (!desc || !st || n_pairs < 0) return 0;
+  return align256((size_t)st->T * sizeof(float2)) + align256((size_t)n_pairs * sizeof(float));
+}
+
+extern "C" size_t mux_pref_workspace_bytes(const mux_pref_desc* desc, const mux_segtab* st) {
+  if (!desc || !st || desc->vocab < 1) return 0;
+  int slabs, slab;
+  cut(desc, slabs, slab);
+  return align256((size_t)n_seqs(st) * sizeof(double)) + align256((size_t)st->T * (size_t)slabs * sizeof(float2));
+}
+
+extern "C" mux_status mux_pref_forward(const mux_pref_desc* desc, const mux_segtab* st, const void* dev_layout, int32_t n_pairs,
+                                       const void* logits, const int32_t* labels, const float* ref_logp, float* row_logp,
+                                       float* logp, float* loss, void* saved, void* ws, size_t ws_bytes, void* hip_stream) {
+  static const char* fn = "mux_pref_forward";
+  if (mux_status s = check(fn, desc, st, n_pairs, false)) return s;
+  if (st->T == 0) return n_pairs == 0 ? MUX_OK : fail(MUX_ERR_SHAPE, std::string(fn) + ": pairs without sequences");
+  if (!dev_layout || !logits || !labels || !ws || (n_pairs > 0 && (!ref_logp || !loss)))
+    return fail(MUX_ERR_INVALID_ARG, std::string(fn) + ": null device pointer");
+  if (ws_bytes < mux_pref_workspace_bytes(desc, st)) return fail(MUX_ERR_WORKSPACE, std::string(fn) + ": workspace too small");
+  const uintptr_t low = (uintptr_t)dev_layout | (uintptr_t)labels | (uintptr_t)ref_logp | (uintptr_t)row_logp | (uintptr_t)logp | (uintptr_t)loss;
+  if ((uintptr_t)logits % esize(desc) || low % 4 || ((uintptr_t)saved | (uintptr_t)ws) % 8)
+    return fail(MUX_ERR_UNSUPPORTED, std::string(fn) + ": a pointer is not aligned to its element");
+  const size_t ns = (size_t)n_seqs(st) * 4, np = (size_t)n_pairs * 4, nt = (size_t)st->T * 4;
+  const Bytes in[4] = {{logits, extent(desc, st, desc->ld)}, {labels, nt}, {ref_logp, n_pairs > 0 ? ns : 0}, {dev_layout, mux_pref_layout_bytes(st, n_pairs)}};
+  const Bytes out[5] = {{row_logp, nt}, {logp, ns}, {loss, np}, {saved, mux_pref_saved_bytes(desc, st, n_pairs)}, {ws, mux_pref_workspace_bytes(desc, st)}};
+  for (int i = 0; i < 5; ++i) {
+    bool bad = false;
+    for (const Bytes& b : in) bad = bad || overlap(out[i].p, out[i].n, b.p, b.n);
+    for (int j = 0; j < i; ++j) bad = bad || overlap(out[i].p, out[i].n, out[j].p, out[j].n);
+    if (bad) return fail(MUX_ERR_INVALID_ARG, std::string(fn) + ": an output overlaps an input or another output");
+  }
+  hipStream_t stream = (hipStream_t)hip_stream;
+  PrefParams p{};
+  p.layout = (const int32_t*)dev_layout;
+  p.logits = logits; p.labels = labels; p.ref = ref_logp;
+  p.row_logp = row_logp; p.logp = logp; p.loss = loss;
+  p.T = st->T; p.V = desc->vocab; p.n_seqs = n_seqs(st); p.n_pairs = n_pairs;
+  cut(desc, p.slabs, p.slab);
+  p.seq_logp = (double*)ws;
+  p.part = (float2*)((char*)ws + align256((size_t)p.n_seqs * sizeof(double)));
+  if (saved) {
+    p.stat = (float2*)saved;
+    p.slope = (float*)((char*)saved + align256((size_t)st->T * sizeof(float2)));
+  }
+  p.ld = desc->ld;
+  const dim3 grid((unsigned)p.T * (unsigned)p.slabs);
+  const unsigned clear = row_logp && st->valid_total < st->T ? (unsigned)((st->T + 1023) / 1024) : 0;
+  const dim3 seqs((unsigned)p.n_seqs + clear);
+  if (desc->dtype == MUX_DT_F32) {
+    MUX_LAUNCH("pref_rows", k_pref_rows<float>, grid, dim3(kThreads), 0, stream, p);
+    MUX_LAUNCH("pref_seqs", k_pref_seqs<float>, seqs, dim3(1024), 0, stream, p);
+  } else {
+    MUX_LAUNCH("pref_rows", k_pref_rows<bf16_t>, grid, dim3(kThreads), 0, stream, p);
+    MUX_LAUNCH("pref_seqs", k_pref_seqs<bf16_t>, seqs, dim3(1024), 0, stream, p);
+  }
+  if (n_pairs > 0) MUX_LAUNCH("pref_pairs", k_pref_pairs, dim3((unsigned)(n_pairs + 255) / 256), dim3(256), 0, stream, p);
+  return last_hip(fn);
+}
+
+extern "C" mux_status mux_pref_backward(const mux_pref_desc* desc, const mux_segtab* st, const void* dev_layout, int32_t n_pairs,
+                                        const void* logits, const int32_t* labels, const void* saved, const float* dloss,
+                                        void* dlogits, void* hip_stream) {
+  static const char* fn = "mux_pref_backward";
+  if (mux_status s = check(fn, desc, st, n_pairs, true)) return s;
+  if (st->T == 0) return n_pairs == 0 ? MUX_OK : fail(MUX_ERR_SHAPE, std::string(fn) + ": pairs without sequences");
+  if (!dev_layout || !logits || !labels || !saved || !dlogits || (n_pairs > 0 && !dloss))
+    return fail(MUX_ERR_INVALID_ARG, std::string(fn) + ": null device pointer");
+  const size_t e = esize(desc), nl = extent(desc, st, desc->ld), ng = extent(desc, st, desc->ldg);
+  if (((uintptr_t)logits | (uintptr_t)dlogits) % e || ((uintptr_t)dev_layout | (uintptr_t)labels | (uintptr_t)dloss) % 4 || (uintptr_t)saved % 8)
+    return fail(MUX_ERR_UNSUPPORTED, std::string(fn) + ": a pointer is not aligned to its element");
+  if ((overlap(dlogits, ng, logits, nl) && !(dlogits == logits && desc->ld == desc->ldg)) ||
+      overlap(dlogits, ng, labels, (size_t)st->T * 4) || overlap(dlogits, ng, saved, mux_pref_saved_bytes(desc, st, n_pairs)) ||
+      overlap(dlogits, ng, dloss, (size_t)n_pairs * 4) || overlap(dlogits, ng, dev_layout, mux_pref_layout_bytes(st, n_pairs)))
+    return fail(MUX_ERR_INVALID_ARG, std::string(fn) + ": dlogits overlaps an input");
+  hipStream_t stream = (hipStream_t)hip_stream;
+  PrefParams p{};
+  p.layout = (const int32_t*)dev_layout;
+  p.logits = logits; p.labels = labels; p.dloss = dloss; p.dlogits = dlogits;
+  p.T = st->T; p.V = desc->vocab; p.n_seqs = n_seqs(st); p.n_pairs = n_pairs;
+  p.ld = desc->ld; p.ldg = desc->ldg;
+  cut(desc, p.slabs, p.slab);
+  p.stat = (float2*)saved;
+  p.slope = (float*)((char*)saved + align256((size_t)st->T * sizeof(float2)));
+  const bool same = (((uintptr_t)logits ^ (uintptr_t)dlogits) & 15) == 0 && ((desc->ld - desc->ldg) * (int64_t)e) % 16 == 0;
+  const dim3 grid((unsigned)p.T * (unsigned)p.slabs);
+  if (desc->dtype == MUX_DT_F32) {
+    if (same) MUX_LAUNCH("pref_bwd", (k_pref_bwd<float, true>), grid, dim3(kThreads), 0, stream, p);
+    else MUX_LAUNCH("pref_bwd", (k_pref_bwd<float, false>), grid, dim3(kThreads), 0, stream, p);
+  } else {
+    if (same) MUX_LAUNCH("pref_bwd", (k_pref_bwd<bf16_t, true>), grid, dim3(kThreads), 0, stream, p);
+    else MUX_LAUNCH("pref_bwd", (k_pref_bwd<bf16_t, false>), grid, dim3(kThreads), 0, stream, p);
+  }
+  return last_hip(fn);
+}
