@@ -55,6 +55,25 @@ mux_status mux_attn_backward(const mux_attn_desc* desc, const mux_segtab* st, co
                              const void* K, const void* V, const void* O, const void* dO, const void* saved, void* dQ,
                              void* dK, void* dV, void* ws, size_t ws_bytes, void* hip_stream);
 
+/* The same attention through a sliding window: token i of a sequence sees token j <= i iff i - j < window or j < n_sinks, the
+ * first tokens staying visible to all (window >= 1, 0 <= n_sinks <= MUX_ATTN_MAX_SINKS).
+ *     O_i = sum_j softmax_j(scale * q_i . k_j) v_j     over the tokens j that i sees
+ * A token always sees itself, so no row is empty.  Descriptor, tensors, padding and types are those of mux_attn_forward and
+ * mux_attn_backward, as are `saved` (mux_attn_saved_bytes) and its use; where no sequence is longer than the window the results
+ * are theirs bit for bit.  Keys outside a row's window take no part in its sums; their values V have to be finite all the
+ * same (0 times an infinity is not 0), as with tokens that causality hides.  The backward's workspace is
+ * mux_attn_window_workspace_bytes() bytes, 16-byte aligned: sum_d dO * O, and, where sequences are longer than the window, partial
+ * sums of the first tokens' dK and dV, which collect contributions of the whole sequence. */
+#define MUX_ATTN_MAX_SINKS 64
+size_t mux_attn_window_workspace_bytes(const mux_attn_desc* desc, int32_t window, int32_t n_sinks, const mux_segtab* st);
+mux_status mux_attn_window_forward(const mux_attn_desc* desc, int32_t window, int32_t n_sinks, const mux_segtab* st,
+                                   const void* dev_segtab, const void* Q, const void* K, const void* V, void* O, void* saved,
+                                   void* hip_stream);
+mux_status mux_attn_window_backward(const mux_attn_desc* desc, int32_t window, int32_t n_sinks, const mux_segtab* st,
+                                    const void* dev_segtab, const void* Q, const void* K, const void* V, const void* O,
+                                    const void* dO, const void* saved, void* dQ, void* dK, void* dV, void* ws, size_t ws_bytes,
+                                    void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -17,11 +17,21 @@ from typing import Dict, Optional, Sequence, Tuple
 import numpy as np
 
 
-def _probabilities(q: np.ndarray, k: np.ndarray, scale: float) -> Tuple[np.ndarray, np.ndarray]:
-    """Row-wise softmax of the causally masked scores of one sequence and head; also the log of each row's sum."""
+def visible(n: int, window: Optional[int] = None, n_sinks: int = 0) -> np.ndarray:
+    """[i, j]: key j is visible to query i iff j <= i and, with a window, i - j < window or j < n_sinks."""
+    v = np.tril(np.ones((n, n), dtype=bool))
+    if window is not None:
+        i, j = np.indices((n, n))
+        v &= (i - j < window) | (j < n_sinks)
+    return v
+
+
+def _probabilities(q: np.ndarray, k: np.ndarray, scale: float, window: Optional[int] = None,
+                   n_sinks: int = 0) -> Tuple[np.ndarray, np.ndarray]:
+    """Row-wise softmax of the masked scores of one sequence and head; also the log of each row's sum."""
     n = q.shape[0]
     s = scale * (q @ k.T)
-    s = np.where(np.tril(np.ones((n, n), dtype=bool)), s, -np.inf)       # key j is visible to query i iff j <= i
+    s = np.where(visible(n, window, n_sinks), s, -np.inf)
     m = s.max(axis=1, keepdims=True)
     e = np.exp(s - m)
     z = e.sum(axis=1, keepdims=True)
@@ -29,7 +39,7 @@ def _probabilities(q: np.ndarray, k: np.ndarray, scale: float) -> Tuple[np.ndarr
 
 
 def forward(Q, K, V, seqs: Sequence[Tuple[int, int]], n_heads: int, scale: Optional[float] = None,
-            n_kv_heads: Optional[int] = None) -> Dict[str, np.ndarray]:
+            n_kv_heads: Optional[int] = None, window: Optional[int] = None, n_sinks: int = 0) -> Dict[str, np.ndarray]:
     Q, K, V = (np.asarray(a, dtype=np.float64) for a in (Q, K, V))
     T, HD = Q.shape
     d = HD // n_heads
@@ -42,14 +52,14 @@ def forward(Q, K, V, seqs: Sequence[Tuple[int, int]], n_heads: int, scale: Optio
         for h in range(n_heads):
             c = slice(h * d, (h + 1) * d)
             ck = slice((h // group) * d, (h // group + 1) * d)
-            p, l = _probabilities(Q[r, c], K[r, ck], scale)
+            p, l = _probabilities(Q[r, c], K[r, ck], scale, window, n_sinks)
             O[r, c] = p @ V[r, ck]
             lse[h, r] = l
     return {"O": O, "lse": lse}
 
 
 def backward(Q, K, V, dO, seqs: Sequence[Tuple[int, int]], n_heads: int, scale: Optional[float] = None,
-             n_kv_heads: Optional[int] = None) -> Dict[str, np.ndarray]:
+             n_kv_heads: Optional[int] = None, window: Optional[int] = None, n_sinks: int = 0) -> Dict[str, np.ndarray]:
     """Gradients of sum(O * dO): with P the probabilities, dV = P^T dO, dP = dO V^T,
     dS = P * (dP - rowsum(dP * P)) (softmax), dQ = scale dS K, dK = scale dS^T Q; a key/value head collects the
     contributions of every query head of its group."""
@@ -64,7 +74,7 @@ def backward(Q, K, V, dO, seqs: Sequence[Tuple[int, int]], n_heads: int, scale: 
         for h in range(n_heads):
             c = slice(h * d, (h + 1) * d)
             ck = slice((h // group) * d, (h // group + 1) * d)
-            p, _ = _probabilities(Q[r, c], K[r, ck], scale)
+            p, _ = _probabilities(Q[r, c], K[r, ck], scale, window, n_sinks)
             dV[r, ck] += p.T @ dO[r, c]
             dp = dO[r, c] @ V[r, ck].T
             ds = p * (dp - (dp * p).sum(axis=1, keepdims=True))

@@ -24,6 +24,7 @@ __all__ = [
     "CostModel", "mux_plan_stage_latency", "mux_plan_htask_latency", "mux_plan_fusion",
     "mux_dispatch_gather", "mux_dispatch_scatter",
     "AttnDesc", "mux_attn_saved_bytes", "mux_attn_workspace_bytes", "mux_attn_forward", "mux_attn_backward",
+    "MUX_ATTN_MAX_SINKS", "mux_attn_window_workspace_bytes", "mux_attn_window_forward", "mux_attn_window_backward",
     "NormDesc", "MUX_NORM_MAX_WIDTH", "mux_norm_saved_bytes", "mux_norm_workspace_bytes", "mux_norm_forward", "mux_norm_backward",
     "PrefDesc", "mux_pref_layout_bytes", "mux_pref_layout", "mux_pref_saved_bytes", "mux_pref_workspace_bytes",
     "mux_pref_forward", "mux_pref_backward",
@@ -39,6 +40,7 @@ MUX_LAYER_REFERENCE_KERNELS = 1
 MUX_MAX_RANK = 64
 MUX_STATIC_WS_BYTES = 32 << 20
 MUX_NORM_MAX_WIDTH = 32768
+MUX_ATTN_MAX_SINKS = 64
 
 _STATUS_NAMES = {1: "MUX_ERR_INVALID_ARG", 2: "MUX_ERR_SHAPE", 3: "MUX_ERR_UNSUPPORTED", 4: "MUX_ERR_WORKSPACE",
                  5: "MUX_ERR_HOST_NOMEM", 6: "MUX_ERR_DEVICE"}
@@ -212,6 +214,10 @@ def load_library() -> ctypes.CDLL:
         "mux_attn_workspace_bytes": (c_size_t, [POINTER(_AttnDescC), vp]),
         "mux_attn_forward": (c_int, [POINTER(_AttnDescC), vp, vp, vp, vp, vp, vp, vp, vp]),
         "mux_attn_backward": (c_int, [POINTER(_AttnDescC), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, c_size_t, vp]),
+        "mux_attn_window_workspace_bytes": (c_size_t, [POINTER(_AttnDescC), c_int32, c_int32, vp]),
+        "mux_attn_window_forward": (c_int, [POINTER(_AttnDescC), c_int32, c_int32, vp, vp, vp, vp, vp, vp, vp, vp]),
+        "mux_attn_window_backward": (c_int, [POINTER(_AttnDescC), c_int32, c_int32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp,
+                                             c_size_t, vp]),
         "mux_norm_saved_bytes": (c_size_t, [POINTER(_NormDescC), vp]),
         "mux_norm_workspace_bytes": (c_size_t, [POINTER(_NormDescC), vp]),
         "mux_norm_forward": (c_int, [POINTER(_NormDescC), vp, vp, vp, vp, vp, vp]),
@@ -579,6 +585,22 @@ def mux_attn_backward(desc: AttnDesc, st: SegTab, dev_segtab, Q, K, V, O, dO, sa
     _check(load_library().mux_attn_backward(ctypes.byref(desc.c), st.handle, _ptr(dev_segtab), _ptr(Q), _ptr(K), _ptr(V),
                                             _ptr(O), _ptr(dO), _ptr(saved), _ptr(dQ), _ptr(dK), _ptr(dV), _ptr(ws),
                                             int(ws_bytes), _stream(stream)))
+
+
+def mux_attn_window_workspace_bytes(desc: AttnDesc, window: int, n_sinks: int, st: SegTab) -> int:
+    return int(load_library().mux_attn_window_workspace_bytes(ctypes.byref(desc.c), int(window), int(n_sinks), st.handle))
+
+
+def mux_attn_window_forward(desc: AttnDesc, window: int, n_sinks: int, st: SegTab, dev_segtab, Q, K, V, O, saved, stream=None) -> None:
+    _check(load_library().mux_attn_window_forward(ctypes.byref(desc.c), int(window), int(n_sinks), st.handle, _ptr(dev_segtab),
+                                                  _ptr(Q), _ptr(K), _ptr(V), _ptr(O), _ptr(saved), _stream(stream)))
+
+
+def mux_attn_window_backward(desc: AttnDesc, window: int, n_sinks: int, st: SegTab, dev_segtab, Q, K, V, O, dO, saved, dQ, dK,
+                             dV, ws, ws_bytes: int, stream=None) -> None:
+    _check(load_library().mux_attn_window_backward(ctypes.byref(desc.c), int(window), int(n_sinks), st.handle, _ptr(dev_segtab),
+                                                   _ptr(Q), _ptr(K), _ptr(V), _ptr(O), _ptr(dO), _ptr(saved), _ptr(dQ), _ptr(dK),
+                                                   _ptr(dV), _ptr(ws), int(ws_bytes), _stream(stream)))
 
 
 def mux_norm_saved_bytes(desc: NormDesc, st: SegTab) -> int:

@@ -54,7 +54,13 @@ struct AttnParams {
   int block0, n_blocks;   // the launch covers the entries block0 .. block0 + n_blocks - 1 of its list
   float scale;        // (comes with the arguments before it: behind the next two, a load of its own that the loops waited for, 41.9 us, 41.6)
   int n_blocks64, grid128;   // one-kernel backward: then as many of at most 64 tokens, from workgroup grid128 on
+  int window, n_sinks;       // WIN kernels: query i sees key j <= i iff i - j < window or j < n_sinks
+  float* sinks;              // WIN backward: partial dK, dV of the first keys from far queries (see k_attn_sink_kv), null: none
 };
+// Whether a query sees the key `ahead` tokens before it
+__device__ __forceinline__ bool in_window(const AttnParams& p, int ahead, bool sink) {
+  return (unsigned)ahead < (unsigned)p.window || (sink && ahead >= 0);
+}
 
 __device__ __forceinline__ bf16x4 lds_read_tr(const bf16_t* p) {
   return __builtin_amdgcn_ds_read_tr16_b64_v4bf16((__attribute__((address_space(3))) bf16x4*)p);
@@ -81,6 +87,12 @@ __device__ __forceinline__ bf16x8 read_across(const bf16_t* tile, int row0, int 
   const bf16_t* p = tile + (row0 + 4 * (grp >> 1) + (j >> 2)) * TP + c0 + 16 * (grp & 1) + 4 * (j & 3);
   const bf16x4 lo = lds_read_tr(p), hi = lds_read_tr(p + 8 * TP);
   return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+// What a wave's lanes wrote to LDS before is there for its lanes' reads after (a wave's LDS accesses stay in their order; the
+// compiler is told not to move them)
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
 }
 // token of accumulator element j for half-wave h inside a 32-token tile
 __device__ __forceinline__ int tok(int j, int half) { return 8 * (j >> 2) + 4 * half + (j & 3); }
@@ -174,8 +186,12 @@ __device__ __forceinline__ void zero_pad_columns(bf16_t* tile, int rows, int pit
   }
 }
 
+// First tile of the keys that the window of some query from q0 on begins in
+__device__ __forceinline__ int window_tile(const AttnParams& p, int q0) { return max(0, q0 - p.window + 1) & ~(TILE - 1); }
+
 // ------------------------------------------------------------------------------------------------ forward
-template <int D>
+// WIN: the query block walks the tile of the first keys (where some are always visible) and then those of its window.
+template <int D, bool WIN>
 __global__ __launch_bounds__(256, 2) void k_attn_fwd(AttnParams p) {
   constexpr int KS = Dim<D>::KS, DT = Dim<D>::DT, DP = Dim<D>::DP, KP = Dim<D>::KP, TP = Dim<D>::TP;
   __shared__ __align__(16) bf16_t sK[TILE * KP];
@@ -208,18 +224,22 @@ __global__ __launch_bounds__(256, 2) void k_attn_fwd(AttnParams p) {
   const int wq_first = q0 + 32 * wave, wq_last = wq_first + 31;
   TileLoadT<TILE, D> tk, tv;
   const int hck = wi_head / (p.H / p.Hkv) * D;  // this head's key/value columns
-  tk.load(p.K, p.ldk, first, 0, len, hck, tid);
-  tv.load(p.V, p.ldv, first, 0, len, hck, tid);
-  for (int kb = 0; kb < kend; kb += TILE) {
+  const int kwin = WIN ? window_tile(p, q0) : 0, kfirst = WIN && p.n_sinks == 0 ? kwin : 0;
+  tk.load(p.K, p.ldk, first, kfirst, len, hck, tid);
+  tv.load(p.V, p.ldv, first, kfirst, len, hck, tid);
+  for (int kb = kfirst, kn; kb < kend; kb = kn) {
+    kn = kb + TILE;
+    if (WIN && kn < kwin) kn = kwin;
     __syncthreads();
     tk.store(sK, KP, tid);
     tv.store(sV, TP, tid);
     __syncthreads();
-    if (kb + TILE < kend) {
-      tk.load(p.K, p.ldk, first, kb + TILE, len, hck, tid);
-      tv.load(p.V, p.ldv, first, kb + TILE, len, hck, tid);
+    if (kn < kend) {
+      tk.load(p.K, p.ldk, first, kn, len, hck, tid);
+      tv.load(p.V, p.ldv, first, kn, len, hck, tid);
     }
     if (kb > wq_last) continue;                 // no key of this tile is visible to this wave's queries
+    if (WIN && kb + TILE <= wq_first - p.window + 1 && kb >= p.n_sinks) continue;
     f32x16 s[2];
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt)
@@ -248,7 +268,17 @@ __global__ __launch_bounds__(256, 2) void k_attn_fwd(AttnParams p) {
     // running maximum on the raw scores (the scale is positive), then one fused multiply-add per element: m is kept in
     // units of the raw score, exp2 arguments are s c - m c
     float mx = -INFINITY;
-    if (diag) {                                 // only the tiles on the diagonal pay for the mask
+    if (WIN && (diag || kb <= wq_last - p.window)) {
+      const int rel = ql - kb - 4 * half, snk = p.n_sinks - kb - 4 * half;
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          const int key = 32 * kt + 8 * (j >> 2) + (j & 3);
+          if (!in_window(p, rel - key, key < snk)) s[kt][j] = -INFINITY;
+        }
+    }
+    if (!WIN && diag) {                         // only the tiles on the diagonal pay for the mask
       const int rel = ql - kb - 4 * half;       // key 32 kt + 8 (j / 4) + j % 4 is hidden iff it exceeds rel
 #pragma unroll
       for (int kt = 0; kt < 2; ++kt)
@@ -380,7 +410,7 @@ __global__ __launch_bounds__(256) void k_attn_delta(AttnParams p) {
 }
 
 // ------------------------------------------------------------------------------------------------ dQ
-template <int D>
+template <int D, bool WIN>
 __global__ __launch_bounds__(256, 2) void k_attn_bwd_q(AttnParams p) {
   constexpr int KS = Dim<D>::KS, DT = Dim<D>::DT, DP = Dim<D>::DP, KP = Dim<D>::KP, TP = Dim<D>::TP;
   __shared__ __align__(16) bf16_t sK[TILE * TP];
@@ -416,18 +446,22 @@ __global__ __launch_bounds__(256, 2) void k_attn_bwd_q(AttnParams p) {
   const int wq_first = q0 + 32 * wave, wq_last = wq_first + 31;
   TileLoadT<TILE, D> tk, tv;
   const int hck = wi_head / (p.H / p.Hkv) * D;  // this head's key/value columns
-  tk.load(p.K, p.ldk, first, 0, len, hck, tid);
-  tv.load(p.V, p.ldv, first, 0, len, hck, tid);
-  for (int kb = 0; kb < kend; kb += TILE) {
+  const int kwin = WIN ? window_tile(p, q0) : 0, kfirst = WIN && p.n_sinks == 0 ? kwin : 0;
+  tk.load(p.K, p.ldk, first, kfirst, len, hck, tid);
+  tv.load(p.V, p.ldv, first, kfirst, len, hck, tid);
+  for (int kb = kfirst, kn; kb < kend; kb = kn) {
+    kn = kb + TILE;
+    if (WIN && kn < kwin) kn = kwin;
     __syncthreads();
     tk.store(sK, TP, tid);
     tv.store(sV, KP, tid);
     __syncthreads();
-    if (kb + TILE < kend) {
-      tk.load(p.K, p.ldk, first, kb + TILE, len, hck, tid);
-      tv.load(p.V, p.ldv, first, kb + TILE, len, hck, tid);
+    if (kn < kend) {
+      tk.load(p.K, p.ldk, first, kn, len, hck, tid);
+      tv.load(p.V, p.ldv, first, kn, len, hck, tid);
     }
     if (kb > wq_last) continue;
+    if (WIN && kb + TILE <= wq_first - p.window + 1 && kb >= p.n_sinks) continue;
     const bool diag = kb + TILE - 1 > wq_first;
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt) {            // one half of the tile at a time keeps the live registers down
@@ -443,7 +477,15 @@ __global__ __launch_bounds__(256, 2) void k_attn_bwd_q(AttnParams p) {
       ATTN_PRIO_LOW();
 #pragma unroll
       for (int j = 0; j < 16; ++j) s[j] = fast_exp2(fmaf(s[j], c, -lse2));        // P^T (zero for a lane without query)
-      if (diag) {                               // only the tiles on the diagonal pay for the mask
+      if (WIN && (diag || kb <= wq_last - p.window)) {
+        const int rel = ql - kb - 32 * kt - 4 * half, snk = p.n_sinks - kb - 32 * kt - 4 * half;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          const int key = 8 * (j >> 2) + (j & 3);
+          if (!in_window(p, rel - key, key < snk)) s[j] = 0.f;
+        }
+      }
+      if (!WIN && diag) {                       // only the tiles on the diagonal pay for the mask
         const int rel = ql - kb - 32 * kt - 4 * half;
 #pragma unroll
         for (int j = 0; j < 16; ++j)
@@ -476,8 +518,134 @@ __global__ __launch_bounds__(256, 2) void k_attn_bwd_q(AttnParams p) {
   }
 }
 
-// ------------------------------------------------------------------------------------------------ dK, dV
+// ------------------------------------------------------------------------------------------------ dK, dV of the first keys
+// Every query of a sequence sees its first n_sinks keys.  What they get from the queries of the first key block's own walk
+// (k_attn_bwd_kv) is formed there; for the rest that walk would be as long as the sequence, one workgroup's while all others walk a
+// window.  So the queries from sink_far on are cut into spans of SINK_SPAN: one workgroup a span, 32 keys and a key/value
+// head, its waves take 32 queries at a time each (no barrier in the loop, tiles of their own in LDS), their sums are
+// added in LDS in a fixed order and the span's fp32 rows go to the workspace, where the first block's workgroup adds them in order.
+constexpr int SINK_SPAN = kAttnSinkSpan * BLK, SINK_TILE = 32;
+__device__ __forceinline__ int sink_far(const AttnParams& p, int len) {       // first query behind the first block's walk
+  return min(len, (BLK - 1 + p.window + SINK_TILE - 1) / SINK_TILE * SINK_TILE);
+}
 template <int D>
+__device__ __forceinline__ size_t sink_part(const AttnParams& p, int slot, int head) {
+  return ((size_t)slot * p.Hkv + head) * (size_t)p.n_sinks * (2 * D);
+}
+template <int D>
+__global__ __launch_bounds__(256, 1) void k_attn_sink_kv(AttnParams p) {
+  constexpr int KS = Dim<D>::KS, DT = Dim<D>::DT, DP = Dim<D>::DP, TP = Dim<D>::TP, QT = SINK_TILE;
+  __shared__ __align__(16) bf16_t tiles[4][2][QT * TP];
+  __shared__ float2 stats[4][QT];
+  static_assert(sizeof(tiles) >= 2 * sizeof(float) * 32 * D, "the sums fit the tiles");
+  const int n_kt = (p.n_sinks + 31) / 32;
+  int wi_block, wi_head;
+  work_item(p.n_blocks, p.Hkv * n_kt, wi_block, wi_head);
+  const int kt = wi_head % n_kt;
+  wi_head /= n_kt;
+  const int32_t* blk = p.dtab + p.list_off + (p.block0 + wi_block) * DA_WORDS;
+  const int first = blk[DA_FIRST_ROW], len = blk[DA_LEN], span0 = blk[DA_BLOCK0];
+  if (span0 % SINK_SPAN != 0) return;
+  const int far = sink_far(p, len), qbegin = max(span0, far), qend = min(len, span0 + SINK_SPAN);
+  if (qbegin >= qend) return;
+  const int hc = wi_head * D, group = p.H / p.Hkv;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, li = lane & 31, half = lane >> 5;
+  const int kl = 32 * kt + li;                 // this lane's key
+  bf16_t *const sQ = tiles[wave][0], *const sD = tiles[wave][1];
+  zero_pad_columns<D, DP, 64>(sQ, QT, TP, lane);
+  zero_pad_columns<D, DP, 64>(sD, QT, TP, lane);
+  bf16x8 kf[KS], vf[KS];
+  {
+    const bool ok = kl < len;
+    const bf16_t* krow = p.K + (size_t)(first + kl) * p.ldk + hc + 8 * half;
+    const bf16_t* vrow = p.V + (size_t)(first + kl) * p.ldv + hc + 8 * half;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      kf[s] = ok ? *(const bf16x8*)(krow + 16 * s) : zero8();
+      vf[s] = ok ? *(const bf16x8*)(vrow + 16 * s) : zero8();
+    }
+  }
+  const float c = p.scale * LOG2E;
+  f32x16 dk[DT], dv[DT];
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int j = 0; j < 16; ++j) { dk[dt][j] = 0.f; dv[dt][j] = 0.f; }
+  for (int g = 0; g < group; ++g) {
+    const int hq = wi_head * group + g, hcq = hq * D;
+    for (int qb = qbegin + QT * wave; qb < qend; qb += 4 * QT) {
+      TileLoadT<QT, D, 64> tq, td;
+      tq.load(p.Q, p.ldq, first, qb, qend, hcq, lane);
+      td.load(p.dO, p.ldo, first, qb, qend, hcq, lane);
+      float2 st = float2{INFINITY, 0.f};       // exp2(x - inf) = 0
+      if (li + qb < qend) {
+        const size_t at = (size_t)hq * p.T + first + qb + li;
+        st = float2{p.lse[at] * LOG2E, p.delta[at]};
+      }
+      wave_sync();
+      tq.store(sQ, TP, lane);
+      td.store(sD, TP, lane);
+      if (half == 0) stats[wave][li] = st;
+      wave_sync();
+      f32x16 s, dp;
+#pragma unroll
+      for (int j = 0; j < 16; ++j) { s[j] = 0.f; dp[j] = 0.f; }
+#pragma unroll
+      for (int k = 0; k < KS; ++k) {
+        s = mma(*(const bf16x8*)(sQ + li * TP + 16 * k + 8 * half), kf[k], s);
+        dp = mma(*(const bf16x8*)(sD + li * TP + 16 * k + 8 * half), vf[k], dp);
+      }
+#pragma unroll
+      for (int j = 0; j < 16; ++j) {           // every query here lies behind the keys: no mask (lanes past n_sinks are not stored)
+        const float2 q = stats[wave][tok(j, half)];
+        s[j] = fast_exp2(fmaf(s[j], c, -q.x));
+        dp[j] = s[j] * (dp[j] - q.y);
+      }
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const bf16x8 pb = pack8(s, u), ds = pack8(dp, u);
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+          dv[dt] = mma(read_across<TP>(sD, 16 * u, 32 * dt, lane), pb, dv[dt]);
+          dk[dt] = mma(read_across<TP>(sQ, 16 * u, 32 * dt, lane), ds, dk[dt]);
+        }
+      }
+    }
+  }
+  // the waves' sums, last wave first; a lane's column of 16 dt values lies 64 lanes apart (no bank twice)
+  __syncthreads();
+  float* sum = (float*)tiles;
+  for (int w = 3; w >= 0; --w) {
+    if (wave == w) {
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          if (32 * dt + 8 * (j >> 2) >= D) continue;
+          float* a = sum + (2 * (16 * dt + j)) * 64 + lane;
+          if (w < 3) { dk[dt][j] += a[0]; dv[dt][j] += a[64]; }
+          if (w > 0) { a[0] = dk[dt][j]; a[64] = dv[dt][j]; }
+        }
+    }
+    __syncthreads();
+  }
+  if (wave == 0 && kl < p.n_sinks) {
+    float* part = p.sinks + sink_part<D>(p, blk[DA_SINK_SLOT] + span0 / SINK_SPAN, wi_head) + (size_t)kl * D + 4 * half;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int jg = 0; jg < 4; ++jg) {
+        if (32 * dt + 8 * jg >= D) continue;
+        *(float4*)(part + 32 * dt + 8 * jg) = float4{dk[dt][4 * jg + 0], dk[dt][4 * jg + 1], dk[dt][4 * jg + 2], dk[dt][4 * jg + 3]};
+        *(float4*)(part + (size_t)p.n_sinks * D + 32 * dt + 8 * jg) =
+            float4{dv[dt][4 * jg + 0], dv[dt][4 * jg + 1], dv[dt][4 * jg + 2], dv[dt][4 * jg + 3]};
+      }
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ dK, dV
+// WIN: a key block walks the queries up to its last key's window; what the first keys get from those beyond comes from k_attn_sink_kv.
+template <int D, bool WIN>
 __global__ __launch_bounds__(256, 2) void k_attn_bwd_kv(AttnParams p) {
   constexpr int KS = Dim<D>::KS, DT = Dim<D>::DT, DP = Dim<D>::DP, KP = Dim<D>::KP, TP = Dim<D>::TP;
   constexpr int QT = 32;                       // queries staged per step
@@ -529,18 +697,20 @@ __global__ __launch_bounds__(256, 2) void k_attn_bwd_kv(AttnParams p) {
   tq.load(p.Q, p.ldq, first, k0, len, hcq, tid);
   td.load(p.dO, p.ldo, first, k0, len, hcq, tid);
   load_stats(k0);
-  for (int qb = k0; qb < len; qb += QT) {       // queries before the block see none of its keys
+  const int qend = WIN ? min(len, k0 + BLK - 1 + p.window) : len;
+  for (int qb = k0; qb < qend; qb += QT) {      // queries before the block see none of its keys
     __syncthreads();
     tq.store(sQ, TP, tid);
     td.store(sD, TP, tid);
     if (tid < QT) { sLse[tid] = r_lse; sDelta[tid] = r_delta; }
     __syncthreads();
-    if (qb + QT < len) {
+    if (qb + QT < qend) {
       tq.load(p.Q, p.ldq, first, qb + QT, len, hcq, tid);
       td.load(p.dO, p.ldo, first, qb + QT, len, hcq, tid);
       load_stats(qb + QT);
     }
     if (qb + QT - 1 < wk_first) continue;     // every query of the tile lies before this wave's keys
+    if (WIN && qb >= wk_first + 31 + p.window && wk_first >= p.n_sinks) continue;
     const bool diag = qb < wk_first + 32;        // some query of the tile lies before some key of the wave
     {
       constexpr int qt = 0;
@@ -556,7 +726,13 @@ __global__ __launch_bounds__(256, 2) void k_attn_bwd_kv(AttnParams p) {
       // P (a lane without key computes on zeros and is not stored)
 #pragma unroll
       for (int j = 0; j < 16; ++j) s[j] = fast_exp2(fmaf(s[j], c, -sLse[32 * qt + tok(j, half)]));
-      if (diag) {                               // only the tiles on the diagonal pay for the mask
+      if (WIN && (diag || qb + QT - 1 - wk_first >= p.window)) {
+        const int rel = kl - qb - 32 * qt - 4 * half;
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+          if (!in_window(p, 8 * (j >> 2) + (j & 3) - rel, kl < p.n_sinks)) s[j] = 0.f;
+      }
+      if (!WIN && diag) {                       // only the tiles on the diagonal pay for the mask
         const int rel = kl - qb - 32 * qt - 4 * half;      // query 8 (j / 4) + j % 4 sees the key iff it is >= rel
 #pragma unroll
         for (int j = 0; j < 16; ++j)
@@ -577,6 +753,21 @@ __global__ __launch_bounds__(256, 2) void k_attn_bwd_kv(AttnParams p) {
     }
   }
   }                                             // next query head of the group
+  if (WIN && p.sinks != nullptr && kl < p.n_sinks) {         // (these keys lie in the first block of their sequence)
+    const int far = sink_far(p, len);
+    for (int b = far / SINK_SPAN * SINK_SPAN; b < len && far < len; b += SINK_SPAN) {
+      const float* part = p.sinks + sink_part<D>(p, blk[DA_SINK_SLOT] + b / SINK_SPAN, wi_head) + (size_t)kl * D + 4 * half;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int jg = 0; jg < 4; ++jg) {
+          if (32 * dt + 8 * jg >= D) continue;
+          const float4 a = *(const float4*)(part + 32 * dt + 8 * jg), v = *(const float4*)(part + (size_t)p.n_sinks * D + 32 * dt + 8 * jg);
+          dk[dt][4 * jg + 0] += a.x; dk[dt][4 * jg + 1] += a.y; dk[dt][4 * jg + 2] += a.z; dk[dt][4 * jg + 3] += a.w;
+          dv[dt][4 * jg + 0] += v.x; dv[dt][4 * jg + 1] += v.y; dv[dt][4 * jg + 2] += v.z; dv[dt][4 * jg + 3] += v.w;
+        }
+    }
+  }
   if (kok) {
     bf16_t* krow = p.dK + (size_t)(first + kl) * p.ldk + hc;
     bf16_t* vrow = p.dV + (size_t)(first + kl) * p.ldv + hc;
@@ -618,7 +809,8 @@ struct ShortLds {
   __align__(16) bf16_t S[R * SP];
   float lse[R], delta[R];
 };
-template <int D, int R>
+// WIN: the mask alone differs (a wave whose keys no query of a step sees forms zeros there).
+template <int D, int R, bool WIN>
 __device__ __forceinline__ void attn_bwd_short(const AttnParams& p, const int wi_block, const int wi_head, const bool stored,
                                                const int tid, ShortLds<D, R>& lds) {
   constexpr int KS = Dim<D>::KS, DT = Dim<D>::DT, DP = Dim<D>::DP, TP = Dim<D>::TP;
@@ -719,7 +911,13 @@ __device__ __forceinline__ void attn_bwd_short(const AttnParams& p, const int wi
         // P (keys past the sequence come after every query: the mask takes them)
 #pragma unroll
         for (int j = 0; j < 16; ++j) s[j] = fast_exp2(fmaf(s[j], c, -sLse[qb + tok(j, half)]));
-        if (qb < 32 * wave + 32) {             // only the tile on the diagonal pays for the mask
+        if (WIN && (qb < 32 * wave + 32 || qb + QT - 1 - 32 * wave >= p.window)) {
+          const int rel = kl - qb - 4 * half;
+#pragma unroll
+          for (int j = 0; j < 16; ++j)
+            if (!in_window(p, 8 * (j >> 2) + (j & 3) - rel, kl < p.n_sinks)) s[j] = 0.f;
+        }
+        if (!WIN && qb < 32 * wave + 32) {     // only the tile on the diagonal pays for the mask
           const int rel = kl - qb - 4 * half;  // query 8 (j / 4) + j % 4 sees the key iff it is >= rel
 #pragma unroll
           for (int j = 0; j < 16; ++j)
@@ -790,7 +988,7 @@ __device__ __forceinline__ void attn_bwd_short(const AttnParams& p, const int wi
 // pass through the dispatcher.  Forward and backward, a launch for each kind, one head a workgroup -> so: 32 heads of 80, 14
 // sequences of 128 tokens and 18 of 64, 62.3 -> 54.4 us; 160 of 64, 224 -> 192; 53 heads of 96, 20 each of 128, 100, 60 and 33
 // tokens, 259 -> 245; 40 heads of 64, the same, 131.8 -> 122.
-template <int D>
+template <int D, bool WIN>
 __global__ __launch_bounds__(256, 2) void k_attn_bwd_short(AttnParams p) {
   typedef ShortLds<D, 128> Wide;
   typedef ShortLds<D, 64> Narrow;
@@ -799,20 +997,20 @@ __global__ __launch_bounds__(256, 2) void k_attn_bwd_short(AttnParams p) {
   int block, head;
   if (blockIdx.x < (unsigned)p.grid128) {
     if (short_item<D>(blockIdx.x, p.n_blocks, p.Hkv, block, head))
-      attn_bwd_short<D, 128>(p, block, head, true, threadIdx.x, *(Wide*)mem);
+      attn_bwd_short<D, 128, WIN>(p, block, head, true, threadIdx.x, *(Wide*)mem);
   } else if (short_item<D>(blockIdx.x - p.grid128, p.n_blocks64, (p.Hkv + 1) / 2, block, head)) {
     const int unit = threadIdx.x >> 7, h = 2 * head + unit;
-    attn_bwd_short<D, 64>(p, p.n_blocks + block, h < p.Hkv ? h : p.Hkv - 1, h < p.Hkv, threadIdx.x & 127, ((Narrow*)mem)[unit]);
+    attn_bwd_short<D, 64, WIN>(p, p.n_blocks + block, h < p.Hkv ? h : p.Hkv - 1, h < p.Hkv, threadIdx.x & 127, ((Narrow*)mem)[unit]);
   }
 }
 // One head a workgroup: D = 128 (two heads of 64 tokens would take 87 KB of LDS, one workgroup a unit; a launch for each kind), and
 // launches of few heads.
-template <int D, int R>
+template <int D, int R, bool WIN>
 __global__ __launch_bounds__(2 * R, 2) void k_attn_bwd_short_one(AttnParams p) {
   __shared__ ShortLds<D, R> lds;
   int block, head;
   if (short_item<D>(blockIdx.x, R == 128 ? p.n_blocks : p.n_blocks64, p.Hkv, block, head))
-    attn_bwd_short<D, R>(p, (R == 128 ? 0 : p.n_blocks) + block, head, true, threadIdx.x, lds);
+    attn_bwd_short<D, R, WIN>(p, (R == 128 ? 0 : p.n_blocks) + block, head, true, threadIdx.x, lds);
 }
 
 mux_status check(const char* fn, const mux_attn_desc* d, const mux_segtab* st) {
@@ -844,6 +1042,25 @@ bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
     else if ((D) == 96) MUX_LAUNCH(name, K<96>, grid, dim3(256), 0, stream, p);            \
     else if ((D) == 80) MUX_LAUNCH(name, K<80>, grid, dim3(256), 0, stream, p);            \
     else MUX_LAUNCH(name, K<64>, grid, dim3(256), 0, stream, p);                           \
+  } while (0)
+// The same of K<D, WIN>.
+#define ATTN_LAUNCH_WIN(name, K, D, win, grid, stream, p)                                  \
+  do {                                                                                     \
+    if ((D) == 128 && (win)) MUX_LAUNCH(name, (K<128, true>), grid, dim3(256), 0, stream, p);   \
+    else if ((D) == 128) MUX_LAUNCH(name, (K<128, false>), grid, dim3(256), 0, stream, p);      \
+    else if ((D) == 96 && (win)) MUX_LAUNCH(name, (K<96, true>), grid, dim3(256), 0, stream, p); \
+    else if ((D) == 96) MUX_LAUNCH(name, (K<96, false>), grid, dim3(256), 0, stream, p);        \
+    else if ((D) == 80 && (win)) MUX_LAUNCH(name, (K<80, true>), grid, dim3(256), 0, stream, p); \
+    else if ((D) == 80) MUX_LAUNCH(name, (K<80, false>), grid, dim3(256), 0, stream, p);        \
+    else if (win) MUX_LAUNCH(name, (K<64, true>), grid, dim3(256), 0, stream, p);               \
+    else MUX_LAUNCH(name, (K<64, false>), grid, dim3(256), 0, stream, p);                       \
+  } while (0)
+// K<args, win>, the template arguments in parentheses
+#define ATTN_ARGS(...) __VA_ARGS__
+#define ATTN_SHORT(name, K, args, grid, block)                                             \
+  do {                                                                                     \
+    if (win) MUX_LAUNCH(name, (K<ATTN_ARGS args, true>), grid, block, 0, stream, p);       \
+    else MUX_LAUNCH(name, (K<ATTN_ARGS args, false>), grid, block, 0, stream, p);          \
   } while (0)
 // Workgroups of a launch whose pairs short_item hands out
 unsigned short_grid(int n_blocks, int n_heads, int D) {
@@ -909,10 +1126,23 @@ extern "C" size_t mux_attn_workspace_bytes(const mux_attn_desc* desc, const mux_
   return mux_attn_saved_bytes(desc, st);
 }
 
-extern "C" mux_status mux_attn_forward(const mux_attn_desc* desc, const mux_segtab* st, const void* dev_segtab,
-                                       const void* Q, const void* K, const void* V, void* O, void* saved,
-                                       void* hip_stream) {
-  static const char* fn = "mux_attn_forward";
+namespace {
+
+// What a query may see beside causality: keys less than `window` tokens back (0: all of them) and the first n_sinks.
+struct Window { int window, n_sinks; };
+
+mux_status check_window(const char* fn, int32_t window, int32_t n_sinks) {
+  if (window < 1 || n_sinks < 0) return fail(MUX_ERR_INVALID_ARG, std::string(fn) + ": window must be positive, n_sinks not negative");
+  if (n_sinks > MUX_ATTN_MAX_SINKS) return fail(MUX_ERR_UNSUPPORTED, std::string(fn) + ": n_sinks above MUX_ATTN_MAX_SINKS");
+  return MUX_OK;
+}
+// A window that no sequence is longer than hides nothing.
+Window effective(const mux_segtab* st, int32_t window, int32_t n_sinks) {
+  return st && window < st->attn_longest ? Window{window, n_sinks} : Window{0, 0};
+}
+
+mux_status forward(const char* fn, const mux_attn_desc* desc, Window w, const mux_segtab* st, const void* dev_segtab, const void* Q,
+                   const void* K, const void* V, void* O, void* saved, void* hip_stream) {
   if (mux_status s = check(fn, desc, st)) return s;
   if (st->T == 0) return MUX_OK;
   if (!dev_segtab || !Q || !K || !V || !O) return fail(MUX_ERR_INVALID_ARG, std::string(fn) + ": null device pointer");
@@ -940,16 +1170,21 @@ extern "C" mux_status mux_attn_forward(const mux_attn_desc* desc, const mux_segt
   // contiguous runs 75.8, blocks dealt in turn 60.0).
   p.short_map = st->n_attn_blocks64 + st->n_attn_blocks128 == st->n_attn_blocks && p.H % 8 == 0 &&
                 (D % 64 != 0 || p.H > p.Hkv || (int64_t)st->n_attn_blocks * p.H >= 8 * kComputeUnits);
+  p.window = w.window; p.n_sinks = w.n_sinks;
   if (st->n_attn_blocks > 0)
-    ATTN_LAUNCH("attn_fwd", k_attn_fwd, D, dim3((unsigned)st->n_attn_blocks * (unsigned)desc->n_heads), stream, p);
+    ATTN_LAUNCH_WIN("attn_fwd", k_attn_fwd, D, w.window > 0, dim3((unsigned)st->n_attn_blocks * (unsigned)desc->n_heads), stream, p);
   return last_hip(fn);
 }
 
-extern "C" mux_status mux_attn_backward(const mux_attn_desc* desc, const mux_segtab* st, const void* dev_segtab,
-                                        const void* Q, const void* K, const void* V, const void* O, const void* dO,
-                                        const void* saved, void* dQ, void* dK, void* dV, void* ws, size_t ws_bytes,
-                                        void* hip_stream) {
-  static const char* fn = "mux_attn_backward";
+// Bytes of the partial dK, dV of the first keys (see k_attn_sink_kv), behind the fp32 [n_heads][T] of the workspace.
+size_t sink_bytes(const mux_attn_desc* desc, const mux_segtab* st, Window w) {
+  if (w.n_sinks == 0 || st->attn_longest <= kAttnBlockRows - 1 + w.window) return 0;
+  return align256((size_t)st->n_attn_spans * (size_t)desc->n_kv_heads * (size_t)w.n_sinks * 2 * (size_t)desc->head_dim * sizeof(float));
+}
+
+mux_status backward(const char* fn, const mux_attn_desc* desc, Window w, const mux_segtab* st, const void* dev_segtab, const void* Q,
+                    const void* K, const void* V, const void* O, const void* dO, const void* saved, void* dQ, void* dK, void* dV,
+                    void* ws, size_t ws_bytes, void* hip_stream) {
   if (mux_status s = check(fn, desc, st)) return s;
   if (st->T == 0) return MUX_OK;
   if (!dev_segtab || !Q || !K || !V || !O || !dO || !saved || !dQ || !dK || !dV || !ws)
@@ -957,7 +1192,7 @@ extern "C" mux_status mux_attn_backward(const mux_attn_desc* desc, const mux_seg
   const void* ptrs[8] = {Q, K, V, O, dO, dQ, dK, dV};
   for (const void* q : ptrs)
     if (!aligned16(q)) return fail(MUX_ERR_UNSUPPORTED, std::string(fn) + ": pointers must be 16-byte aligned");
-  if (ws_bytes < mux_attn_workspace_bytes(desc, st)) return fail(MUX_ERR_WORKSPACE, std::string(fn) + ": workspace too small");
+  if (ws_bytes < mux_attn_workspace_bytes(desc, st) + sink_bytes(desc, st, w)) return fail(MUX_ERR_WORKSPACE, std::string(fn) + ": workspace too small");
   hipStream_t stream = (hipStream_t)hip_stream;
   const int D = desc->head_dim;
   AttnParams p{};
@@ -977,22 +1212,29 @@ extern "C" mux_status mux_attn_backward(const mux_attn_desc* desc, const mux_seg
   int n64 = 0, n128 = 0, n_long = 0;
   plan_backward(st, desc, n_long, n128, n64);
   p.list_off = st->dev_image[DH_ATT_OFF_BWD];
+  const bool win = w.window > 0;
+  p.window = w.window; p.n_sinks = w.n_sinks;
   if (n_long > 0) {
     const size_t n = (size_t)st->T * desc->n_heads;
     p.n_blocks = n_long;
     ATTN_LAUNCH("attn_delta", k_attn_delta, D, dim3((unsigned)(((n + 3) / 4 * 16 + 255) / 256)), stream, p);
-    ATTN_LAUNCH("attn_bwd_kv", k_attn_bwd_kv, D, dim3((unsigned)n_long * (unsigned)desc->n_kv_heads), stream, p);
+    if (sink_bytes(desc, st, w) > 0) {
+      if ((uintptr_t)ws % 16) return fail(MUX_ERR_UNSUPPORTED, std::string(fn) + ": the workspace must be 16-byte aligned");
+      p.sinks = (float*)((char*)ws + mux_attn_workspace_bytes(desc, st));
+      ATTN_LAUNCH("attn_sink_kv", k_attn_sink_kv, D, dim3((unsigned)n_long * (unsigned)(desc->n_kv_heads * ((w.n_sinks + 31) / 32))), stream, p);
+    }
+    ATTN_LAUNCH_WIN("attn_bwd_kv", k_attn_bwd_kv, D, win, dim3((unsigned)n_long * (unsigned)desc->n_kv_heads), stream, p);
     AttnParams q = p;
     q.list_off = st->dev_image[DH_ATT_OFF_FWD];
-    ATTN_LAUNCH("attn_bwd_q", k_attn_bwd_q, D, dim3((unsigned)n_long * (unsigned)desc->n_heads), stream, q);
+    ATTN_LAUNCH_WIN("attn_bwd_q", k_attn_bwd_q, D, win, dim3((unsigned)n_long * (unsigned)desc->n_heads), stream, q);
   }
   if (n128 + n64 > 0) {
     p.block0 = n_long;
     p.n_blocks = n128; p.n_blocks64 = n64;
     const unsigned one64 = n64 > 0 ? short_grid(n64, desc->n_kv_heads, D) : 0;
     if (D == 128) {
-      if (n128 > 0) MUX_LAUNCH("attn_bwd_128", (k_attn_bwd_short_one<128, 128>), dim3(short_grid(n128, desc->n_kv_heads, D)), dim3(256), 0, stream, p);
-      if (n64 > 0) MUX_LAUNCH("attn_bwd_64", (k_attn_bwd_short_one<128, 64>), dim3(one64), dim3(128), 0, stream, p);
+      if (n128 > 0) ATTN_SHORT("attn_bwd_128", k_attn_bwd_short_one, (128, 128), dim3(short_grid(n128, desc->n_kv_heads, D)), dim3(256));
+      if (n64 > 0) ATTN_SHORT("attn_bwd_64", k_attn_bwd_short_one, (128, 64), dim3(one64), dim3(128));
     } else if (n128 == 0 && (int64_t)n64 * desc->n_kv_heads * D < (D == 64 ? 2048 : 1536) * (int64_t)kComputeUnits) {
       // Nothing but sequences of at most 64 tokens: two heads a workgroup move whole lines where there is enough to move
       // (48 MB a tensor of full sequences; 64 MB of heads of 64, whose rows are whole lines); below, a workgroup of twice the
@@ -1000,17 +1242,53 @@ extern "C" mux_status mux_attn_backward(const mux_attn_desc* desc, const mux_seg
       // one head, two: 16 heads of 96, 40 x 50 tokens 45.2 us, 47.7; 40 of 96, 80 x 50 110.4, 115.2; 24 of 96, 160 x 50 119.7,
       // 119.3; 53 of 96, 80 x 50 153.1, 150.5, 160 x 64 358.7, 336.5; 33 of 80, 80 x 64 79.1, 82.6, 160 x 64 190.8, 183.3; 32 of 80, 160 x
       // 64 229.9, 195.9; 40 of 64, 80 x 50 81.9, 86.0, 160 x 50 133.8, 144.8, 300 x 64 362.6, 333.3; 8 groups of 4 heads of 64, 160 x 64 85.7, 92.1.
-      if (D == 96) MUX_LAUNCH("attn_bwd_64", (k_attn_bwd_short_one<96, 64>), dim3(one64), dim3(128), 0, stream, p);
-      else if (D == 80) MUX_LAUNCH("attn_bwd_64", (k_attn_bwd_short_one<80, 64>), dim3(one64), dim3(128), 0, stream, p);
-      else MUX_LAUNCH("attn_bwd_64", (k_attn_bwd_short_one<64, 64>), dim3(one64), dim3(128), 0, stream, p);
+      if (D == 96) ATTN_SHORT("attn_bwd_64", k_attn_bwd_short_one, (96, 64), dim3(one64), dim3(128));
+      else if (D == 80) ATTN_SHORT("attn_bwd_64", k_attn_bwd_short_one, (80, 64), dim3(one64), dim3(128));
+      else ATTN_SHORT("attn_bwd_64", k_attn_bwd_short_one, (64, 64), dim3(one64), dim3(128));
     } else {
       p.grid128 = n128 > 0 ? (int)short_grid(n128, desc->n_kv_heads, D) : 0;
       const char* name = n64 == 0 ? "attn_bwd_128" : (n128 == 0 ? "attn_bwd_64" : "attn_bwd_128_64");
       const dim3 grid((unsigned)p.grid128 + (n64 > 0 ? short_grid(n64, (desc->n_kv_heads + 1) / 2, D) : 0));
-      if (D == 96) MUX_LAUNCH(name, k_attn_bwd_short<96>, grid, dim3(256), 0, stream, p);
-      else if (D == 80) MUX_LAUNCH(name, k_attn_bwd_short<80>, grid, dim3(256), 0, stream, p);
-      else MUX_LAUNCH(name, k_attn_bwd_short<64>, grid, dim3(256), 0, stream, p);
+      if (D == 96) ATTN_SHORT(name, k_attn_bwd_short, (96), grid, dim3(256));
+      else if (D == 80) ATTN_SHORT(name, k_attn_bwd_short, (80), grid, dim3(256));
+      else ATTN_SHORT(name, k_attn_bwd_short, (64), grid, dim3(256));
     }
   }
   return last_hip(fn);
+}
+
+}  // namespace
+
+extern "C" mux_status mux_attn_forward(const mux_attn_desc* desc, const mux_segtab* st, const void* dev_segtab, const void* Q,
+                                       const void* K, const void* V, void* O, void* saved, void* hip_stream) {
+  return forward("mux_attn_forward", desc, Window{0, 0}, st, dev_segtab, Q, K, V, O, saved, hip_stream);
+}
+
+extern "C" mux_status mux_attn_backward(const mux_attn_desc* desc, const mux_segtab* st, const void* dev_segtab, const void* Q,
+                                        const void* K, const void* V, const void* O, const void* dO, const void* saved, void* dQ,
+                                        void* dK, void* dV, void* ws, size_t ws_bytes, void* hip_stream) {
+  return backward("mux_attn_backward", desc, Window{0, 0}, st, dev_segtab, Q, K, V, O, dO, saved, dQ, dK, dV, ws, ws_bytes, hip_stream);
+}
+
+extern "C" size_t mux_attn_window_workspace_bytes(const mux_attn_desc* desc, int32_t window, int32_t n_sinks, const mux_segtab* st) {
+  if (!desc || !st || desc->n_heads < 1 || desc->n_kv_heads < 1 || desc->head_dim < 1 || window < 1 || n_sinks < 0 || n_sinks > MUX_ATTN_MAX_SINKS)
+    return 0;
+  return mux_attn_workspace_bytes(desc, st) + sink_bytes(desc, st, effective(st, window, n_sinks));
+}
+
+extern "C" mux_status mux_attn_window_forward(const mux_attn_desc* desc, int32_t window, int32_t n_sinks, const mux_segtab* st,
+                                              const void* dev_segtab, const void* Q, const void* K, const void* V, void* O,
+                                              void* saved, void* hip_stream) {
+  static const char* fn = "mux_attn_window_forward";
+  if (mux_status s = check_window(fn, window, n_sinks)) return s;
+  return forward(fn, desc, effective(st, window, n_sinks), st, dev_segtab, Q, K, V, O, saved, hip_stream);
+}
+
+extern "C" mux_status mux_attn_window_backward(const mux_attn_desc* desc, int32_t window, int32_t n_sinks, const mux_segtab* st,
+                                               const void* dev_segtab, const void* Q, const void* K, const void* V, const void* O,
+                                               const void* dO, const void* saved, void* dQ, void* dK, void* dV, void* ws,
+                                               size_t ws_bytes, void* hip_stream) {
+  static const char* fn = "mux_attn_window_backward";
+  if (mux_status s = check_window(fn, window, n_sinks)) return s;
+  return backward(fn, desc, effective(st, window, n_sinks), st, dev_segtab, Q, K, V, O, dO, saved, dQ, dK, dV, ws, ws_bytes, hip_stream);
 }

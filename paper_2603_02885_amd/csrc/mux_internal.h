@@ -32,9 +32,10 @@ constexpr uint32_t kDevMagic = 0x4458554Du;  // "MUXD"
 
 // per task, 8 words
 enum : int { DT_ROW_BEGIN = 0, DT_ROW_COUNT, DT_VALID, DT_KIND, DT_RANK, DT_SCALE_BITS, DT_ZROW0, DT_ITEM_PAD, DT_WORDS };
-// per attention block, 4 words: the sequence's first row and length, the block's first token inside the sequence
-enum : int { DA_FIRST_ROW = 0, DA_LEN, DA_BLOCK0, DA_PAD, DA_WORDS };
-constexpr int kAttnBlockRows = 128;
+// per attention block, 4 words: the sequence's first row and length, the block's first token inside the sequence, and in the
+// second list the number of the sequence's first span of kAttnSinkSpan blocks, counted through the sequences
+enum : int { DA_FIRST_ROW = 0, DA_LEN, DA_BLOCK0, DA_SINK_SLOT, DA_WORDS };
+constexpr int kAttnBlockRows = 128, kAttnSinkSpan = 4;
 // per work item, 4 words: rows [row0, row0+nrows) all belong to `task` (-1: rows of no task)
 enum : int { DI_TASK = 0, DI_ROW0, DI_NROWS, DI_NVALID, DI_WORDS };
 
@@ -95,6 +96,7 @@ struct mux_segtab {
   int32_t n_attn_blocks = 0;        // 128-row blocks of sequences (attention work items)
   int32_t n_attn_blocks128 = 0, n_attn_blocks64 = 0;   // those of sequences of 65..128 and of at most 64 tokens (one each)
   int32_t attn_longest = 0;         // tokens of the longest sequence
+  int32_t n_attn_spans = 0;         // spans of kAttnSinkSpan blocks of all sequences
   std::vector<mux::Item> items[mux::kNumTileSizes];
   std::vector<int32_t> task_item_begin[mux::kNumTileSizes], task_item_count[mux::kNumTileSizes];
   // 256-row work items by what the backbone product has to compute of them: those with a real token past their first
