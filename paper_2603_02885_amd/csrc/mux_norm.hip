@@ -3,11 +3,15 @@
 // All of it is bound by memory: about ten operations for the 4 (forward) or 6 bytes (backward) that a bf16 element moves.  A
 // row is held in the registers of the lanes that own it from its first read to its last use, so that mean, squared
 // deviations and the result (backward: both row sums and dX) take one pass over memory and the variance is summed from
-// deviations, not as a difference of two large sums.  A wave owns a row (64 lanes, no barrier); wide rows belong to a workgroup.
-// The gradients of the weights are sums down the columns: a lane keeps those of its columns in registers over the
-// rows of its piece (part of a 64-row work item, so of one task), the waves of a workgroup are added in LDS, and a second launch
+// deviations, not as a difference of two large sums.
+// Forward: a wave owns a row up to 10 pieces of 16 bytes a lane, without barriers.  Backward: the gradients of the weights are sums
+// down the columns, which a lane keeps in registers over the rows of its piece (consecutive rows of one task), so a row is shared
+// by as many waves as leave a lane two pieces and the sums of a piece are 8 N bytes once in some ten rows; a second launch
 // adds the pieces of a task in their order (no atomics: results repeat bit for bit).
+// A lane's 16 bytes need not lie on 16-byte boundaries (memory instructions take any address here): odd widths and leading
+// dimensions run in the same kernels, their last piece element by element.
 #include <algorithm>
+#include <initializer_list>
 #include <new>
 #include <utility>
 
@@ -19,52 +23,73 @@ namespace {
 
 constexpr int kBatch = 32;      // tasks a launch (pointers as kernel arguments)
 
-// VW consecutive elements of a row as they are stored
-template <class S, int VW> struct Piece;
-template <> struct Piece<bf16_t, 8> {
-  uint4 r;
-  __device__ __forceinline__ void load(const bf16_t* p) { r = *(const uint4*)p; }
-  __device__ __forceinline__ void fill(bf16_t one) { const uint32_t v = one | (uint32_t)one << 16; r = uint4{v, v, v, v}; }
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+template <class S> struct Any;  // 16 bytes at any element's address
+template <> struct Any<bf16_t> { typedef u32x4 type __attribute__((aligned(2))); };
+template <> struct Any<float> { typedef u32x4 type __attribute__((aligned(4))); };
+
+// How rows are moved.  WHOLE: they are whole pieces; STREAM: the same, past the caches; ODD: the last piece is part of one.
+enum Mode { WHOLE, STREAM, ODD };
+
+// 16 bytes of a row as they are stored: E elements, of which those from `left` on lie past the row (zero when read, not written).
+template <class S>
+struct Piece {
+  static constexpr int E = 16 / (int)sizeof(S);
+  u32x4 r;
+  __device__ __forceinline__ void fill(S v) {
+    const uint32_t w = sizeof(S) == 2 ? (uint32_t)(bf16_t)v * 0x10001u : __float_as_uint((float)v);
+    r = u32x4{w, w, w, w};
+  }
   __device__ __forceinline__ float get(int i) const {
-    const uint32_t w = i < 2 ? r.x : i < 4 ? r.y : i < 6 ? r.z : r.w;
-    return __uint_as_float(i & 1 ? w & 0xffff0000u : w << 16);
+    if constexpr (sizeof(S) == 4) return __uint_as_float(r[i]);
+    else return __uint_as_float(i & 1 ? r[i >> 1] & 0xffff0000u : r[i >> 1] << 16);
   }
-  static __device__ __forceinline__ void store(bf16_t* p, const float* v) {
-    *(uint4*)p = uint4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+  template <Mode M>
+  __device__ __forceinline__ void load(const S* p, int left) {
+    typedef typename Any<S>::type A;
+    if (M != ODD || left >= E) {
+      if constexpr (M == STREAM) r = __builtin_nontemporal_load((const A*)p);
+      else r = *(const A*)p;
+    } else {
+      float v[E];
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[e] = e < left ? Store<S>::ld(p, e) : 0.f;
+      r = pack(v);
+    }
   }
-};
-template <> struct Piece<bf16_t, 1> {
-  bf16_t r;
-  __device__ __forceinline__ void load(const bf16_t* p) { r = *p; }
-  __device__ __forceinline__ void fill(bf16_t one) { r = one; }
-  __device__ __forceinline__ float get(int) const { return bf16_to_f32(r); }
-  static __device__ __forceinline__ void store(bf16_t* p, const float* v) { *p = f32_to_bf16(v[0]); }
-};
-template <> struct Piece<float, 4> {
-  float4 r;
-  __device__ __forceinline__ void load(const float* p) { r = *(const float4*)p; }
-  __device__ __forceinline__ void fill(float one) { r = float4{one, one, one, one}; }
-  __device__ __forceinline__ float get(int i) const { return i == 0 ? r.x : i == 1 ? r.y : i == 2 ? r.z : r.w; }
-  static __device__ __forceinline__ void store(float* p, const float* v) { *(float4*)p = float4{v[0], v[1], v[2], v[3]}; }
-};
-template <> struct Piece<float, 1> {
-  float r;
-  __device__ __forceinline__ void load(const float* p) { r = *p; }
-  __device__ __forceinline__ void fill(float one) { r = one; }
-  __device__ __forceinline__ float get(int) const { return r; }
-  static __device__ __forceinline__ void store(float* p, const float* v) { *p = v[0]; }
+  static __device__ __forceinline__ u32x4 pack(const float* v) {
+    if constexpr (sizeof(S) == 4) return u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+    else return u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+  }
+  template <Mode M>
+  static __device__ __forceinline__ void store(S* p, const float* v, int left) {
+    typedef typename Any<S>::type A;
+    if (M != ODD || left >= E) {
+      if constexpr (M == STREAM) __builtin_nontemporal_store(pack(v), (A*)p);
+      else *(A*)p = pack(v);
+    } else {
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        if (e < left) Store<S>::st(p, e, v[e]);
+    }
+  }
 };
 template <class S> __device__ __forceinline__ S one_of();
 template <> __device__ __forceinline__ bf16_t one_of<bf16_t>() { return 0x3F80; }
 template <> __device__ __forceinline__ float one_of<float>() { return 1.f; }
 
+// The rows of a launch: ranges of consecutive rows of one task each (the last may be rows of no task), cut into pieces of `rows` rows.
+struct Ranges {
+  int n, rows;
+  int row0[kBatch + 1], row1[kBatch + 1];
+  int piece0[kBatch + 2];   // number of the range's first piece
+};
+
 struct NormParams {
-  const int32_t* dtab;
-  const void* gamma[kBatch];
-  const void* beta[kBatch];
-  int task_base;
-  int item0;                // first 64-row work item of the launch
-  int rows;                 // rows a piece: a power of two up to 64
+  const uint32_t* rowbits;  // of the table: bit i of the whole = row i is a token
+  const void* gamma[kBatch + 1];
+  const void* beta[kBatch + 1];
+  Ranges in;
   int N, T;
   float eps, inv_n;
   int64_t ldx, ldy;
@@ -74,238 +99,267 @@ struct NormParams {
   float* part;              // backward: [piece][2][N] partial sums of dgamma, dbeta, null: not wanted
 };
 
-// The rows of a workgroup: piece `blockIdx.x` of the launch, LPR lanes a row.
-template <int LPR>
+constexpr int kMaxRows = 64;
+
+// What a workgroup takes: the piece's rows and which of them are tokens (bit r: row0 + r), the same in every lane.
 struct Rows {
-  static constexpr int THREADS = LPR == 64 ? 256 : LPR, SUBS = THREADS / LPR;
-  int task, row0, r0, r1;   // rows row0 + r0 .. row0 + r1 - 1, all of `task` (-1: of none)
-  uint64_t valid;           // bit r: row0 + r is a token
-  __device__ __forceinline__ Rows(const NormParams& p) {
-    const int per = 64 / p.rows, item = p.item0 + (int)blockIdx.x / per;
-    const ItemView it = load_item(p.dtab, 0, item);
-    const uint32_t* bits = (const uint32_t*)(p.dtab + p.dtab[DH_OFF_ITEM_BITS]) + 2 * item;
-    task = it.task;
-    row0 = it.row0;
-    r0 = (int)blockIdx.x % per * p.rows;
-    r1 = min(r0 + p.rows, it.nrows);
-    valid = task < 0 ? 0 : (uint64_t)bits[0] | (uint64_t)bits[1] << 32;
+  int range, row0, n;
+  uint64_t valid;
+  static __device__ __forceinline__ uint32_t bits32(const uint32_t* bits, int row) {
+    return (uint32_t)(((uint64_t)bits[row >> 5] | (uint64_t)bits[(row >> 5) + 1] << 32) >> (row & 31));
   }
-  __device__ __forceinline__ bool any() const {      // a token among the piece's rows
-    return r1 > r0 && (valid >> r0 & (~(uint64_t)0 >> (64 - (r1 - r0)))) != 0;
+  __device__ __forceinline__ Rows(const NormParams& p, int piece) {
+    const Ranges& in = p.in;
+    int lo = 0, hi = in.n;                               // the last range that does not begin behind the piece
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (in.piece0[mid] <= piece) lo = mid; else hi = mid;
+    }
+    range = lo;
+    row0 = in.row0[lo] + (piece - in.piece0[lo]) * in.rows;
+    n = min(in.rows, in.row1[lo] - row0);
+    valid = bits32(p.rowbits, row0);
+    if (n > 32) valid |= (uint64_t)bits32(p.rowbits, row0 + 32) << 32;
   }
 };
 
-// Sums over the LPR lanes of a row, the same value in every lane.  `slot` alternates between calls, so that one barrier a call is enough.
-template <int LPR, int COUNT>
-__device__ __forceinline__ void row_sum(float (&v)[COUNT], float (*lds)[COUNT][LPR / 64], int slot) {
-#pragma unroll
-  for (int m = 32; m >= 1; m >>= 1)
-#pragma unroll
-    for (int k = 0; k < COUNT; ++k) v[k] += __shfl_xor(v[k], m);
-  if constexpr (LPR > 64) {
-    if ((threadIdx.x & 63) == 0)
-#pragma unroll
-      for (int k = 0; k < COUNT; ++k) lds[slot][k][threadIdx.x >> 6] = v[k];
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < COUNT; ++k) {
-      float s = 0.f;
-#pragma unroll
-      for (int w = 0; w < LPR / 64; ++w) s += lds[slot][k][w];
-      v[k] = s;
-    }
-  }
+// Sum over the wave, the same in every lane: inside rows of 16 lanes, then across the rows into lane 63.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float dpp_add(float v) {
+  return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, ROWS, 0xf, false));
+}
+__device__ __forceinline__ float wave_sum(float v) {
+  v = dpp_add<0xB1, 0xf>(v);       // lanes 1 apart
+  v = dpp_add<0x4E, 0xf>(v);       // 2 apart
+  v = dpp_add<0x141, 0xf>(v);      // mirrored in halves of a row
+  v = dpp_add<0x140, 0xf>(v);      // mirrored in a row
+  v = dpp_add<0x142, 0xa>(v);      // the row before, into rows 1 and 3
+  v = dpp_add<0x143, 0xc>(v);      // the two rows before, into rows 2 and 3
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
 }
 
-template <class S, int VW, int NV, int LPR>
-__global__ __launch_bounds__(Rows<LPR>::THREADS) void k_norm_fwd(NormParams p) {
-  typedef Piece<S, VW> P;
-  __shared__ float lds[2][1][LPR / 64];
-  const Rows<LPR> rows(p);
-  const int sub = threadIdx.x / LPR, lane = threadIdx.x % LPR;
+// WAVES = 1: a wave has a row of its own and the workgroup four.  More: a row belongs to the workgroup's waves (at most so many).
+// NV: a lane's pieces.  17637 rows of 5120 bf16 values (19968 with padding): 73 us, 5.3 TB/s; 2944 x 2560 9.6 us, 448 x 4096 6.7.
+// (Registers for fewer waves pay: held to three a SIMD 103 us; 8 rows a workgroup 90; through the caches 92.)
+template <class S, int NV, int WAVES, Mode M>
+__global__ __launch_bounds__(WAVES > 1 ? 64 * WAVES : 256, WAVES > 8 ? 4 : 2) void k_norm_fwd(NormParams p) {
+  typedef Piece<S> P;
+  constexpr int E = P::E;
+  constexpr bool WIDE = WAVES > 1;
+  __shared__ float3 part[2][WAVES];                      // a wave's elements, their mean and squared deviations from it
+  const Rows rows(p, blockIdx.x);
+  const int wave = threadIdx.x >> 6, lanes = WIDE ? (int)blockDim.x : 64, lane = WIDE ? (int)threadIdx.x : (int)threadIdx.x & 63;
   const S* X = (const S*)p.X;
   S* Y = (S*)p.Y;
-  P g[NV], b[NV];
-  if (rows.task >= 0) {
-    const S* gp = (const S*)p.gamma[rows.task - p.task_base];
-    const S* bp = (const S*)p.beta[rows.task - p.task_base];
+  const S *gp = (const S*)p.gamma[rows.range], *bp = (const S*)p.beta[rows.range];
+  int mine = 0;                                          // elements of a row that this wave holds
+#pragma unroll
+  for (int i = 0; i < NV; ++i) mine += min(64 * E, max(0, p.N - ((lane & ~63) + i * lanes) * E));
+  const float inv_mine = 1.f / (float)max(mine, 1);
+  int slot = 0;
+  for (int r = WIDE ? 0 : wave; r < rows.n; r += WIDE ? 1 : 4) {
+    const int row = rows.row0 + r;
+    const bool ok = rows.valid >> r & 1;
+    P v[NV], g[NV], b[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int c = (lane + i * LPR) * VW;
+      const int c = (lane + i * lanes) * E;
+      v[i].fill(0);
+      if (ok && c < p.N) v[i].template load<M>(X + (size_t)row * p.ldx + c, p.N - c);
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {                       // (from the caches for all but a task's first rows; asked for behind the sums: 83 us for 73)
+      const int c = (lane + i * lanes) * E;
       g[i].fill(one_of<S>());
       b[i].fill(0);
-      if (gp && c < p.N) g[i].load(gp + c);
-      if (bp && c < p.N) b[i].load(bp + c);
+      if (gp && c < p.N) g[i].template load<M == ODD ? ODD : WHOLE>(gp + c, p.N - c);
+      if (bp && c < p.N) b[i].template load<M == ODD ? ODD : WHOLE>(bp + c, p.N - c);
     }
-  }
-  for (int r = rows.r0 + sub; r < rows.r1; r += Rows<LPR>::SUBS) {
-    const int row = rows.row0 + r;
-    S* y = Y + (size_t)row * p.ldy;
-    if (!(rows.valid >> r & 1)) {
-      const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        const int c = (lane + i * LPR) * VW;
-        if (c < p.N) P::store(y + c, zero);
-      }
-      continue;
-    }
-    const S* x = X + (size_t)row * p.ldx;
-    P v[NV];
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int c = (lane + i * LPR) * VW;
-      v[i].fill(0);
-      if (c < p.N) v[i].load(x + c);
-    }
-    float s[1] = {0.f};
+    float s = 0.f;
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
-      for (int e = 0; e < VW; ++e) s[0] += v[i].get(e);
-    row_sum<LPR, 1>(s, lds, 0);
-    const float mean = s[0] * p.inv_n;
-    s[0] = 0.f;
+      for (int e = 0; e < E; ++e) s += v[i].get(e);
+    float mean = wave_sum(s) * inv_mine;
+    s = 0.f;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      if ((lane + i * LPR) * VW >= p.N) continue;
+      const int left = p.N - (lane + i * lanes) * E;
+      if (M != ODD && left <= 0) continue;
+      if (M != ODD || left >= E) {
 #pragma unroll
-      for (int e = 0; e < VW; ++e) {
-        const float d = v[i].get(e) - mean;
-        s[0] = fmaf(d, d, s[0]);
+        for (int e = 0; e < E; ++e) {
+          const float d = v[i].get(e) - mean;
+          s = fmaf(d, d, s);
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const float d = e < left ? v[i].get(e) - mean : 0.f;
+          s = fmaf(d, d, s);
+        }
       }
     }
-    row_sum<LPR, 1>(s, lds, 1);
-    const float rstd = 1.f / sqrtf(s[0] * p.inv_n + p.eps);
+    float m2 = wave_sum(s);
+    if constexpr (WIDE) {                                // the waves' parts of the row: means weighed, deviations moved to the common one
+      const int waves = (int)blockDim.x >> 6;
+      if ((threadIdx.x & 63) == 0) part[slot][wave] = float3{(float)mine, mean, m2};
+      __syncthreads();
+      s = 0.f;
+      for (int w = 0; w < waves; ++w) s = fmaf(part[slot][w].x, part[slot][w].y, s);
+      mean = s * p.inv_n;
+      m2 = 0.f;
+      for (int w = 0; w < waves; ++w) {
+        const float d = part[slot][w].y - mean;
+        m2 += fmaf(part[slot][w].x * d, d, part[slot][w].z);
+      }
+      slot ^= 1;                                         // (the next row's parts: one barrier a row is enough)
+    }
+    const float rstd = 1.f / sqrtf(m2 * p.inv_n + p.eps);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int c = (lane + i * LPR) * VW;
+      const int c = (lane + i * lanes) * E;
       if (c >= p.N) continue;
-      float o[VW];
+      float o[E];
 #pragma unroll
-      for (int e = 0; e < VW; ++e) o[e] = fmaf((v[i].get(e) - mean) * rstd, g[i].get(e), b[i].get(e));
-      P::store(y + c, o);
+      for (int e = 0; e < E; ++e) o[e] = ok ? fmaf((v[i].get(e) - mean) * rstd, g[i].get(e), b[i].get(e)) : 0.f;
+      P::template store<M>(Y + (size_t)row * p.ldy + c, o, p.N - c);
     }
-    if (p.mean && lane == 0) { p.mean[row] = mean; p.rstd[row] = rstd; }
+    if (p.mean && lane == 0 && ok) { p.mean[row] = mean; p.rstd[row] = rstd; }
   }
 }
 
-template <class S, int VW, int NV, int LPR>
-__global__ __launch_bounds__(Rows<LPR>::THREADS) void k_norm_bwd(NormParams p) {
-  typedef Piece<S, VW> P;
-  constexpr int SUBS = Rows<LPR>::SUBS;
-  __shared__ float lds[2][2][LPR / 64];
-  __shared__ float acc[SUBS > 1 ? 2 : 1][SUBS > 1 ? NV * VW * LPR : 1];
-  const Rows<LPR> rows(p);
-  const int sub = threadIdx.x / LPR, lane = threadIdx.x % LPR;
+// The next row is on its way while this one is summed.  17637 x 5120 bf16: 124 us, 4.6 TB/s, and 10 us for the sum of the pieces
+// (dX through the caches 150, without the next row on its way 159); 2944 x 2560 14.7 and 4.7.
+template <class S, int NV, int WAVES, Mode M>
+__global__ __launch_bounds__(WAVES > 1 ? 64 * WAVES : 256, WAVES > 8 ? 4 : 3) void k_norm_bwd(NormParams p) {
+  typedef Piece<S> P;
+  constexpr int E = P::E;
+  constexpr bool WIDE = WAVES > 1;
+  constexpr int STEP = WIDE ? 1 : 4;
+  __shared__ float2 part[2][WAVES];
+  __shared__ float acc[WIDE ? 1 : 2][WIDE ? 1 : NV * E * 64];
+  const Rows rows(p, blockIdx.x);
+  const int wave = threadIdx.x >> 6, lanes = WIDE ? (int)blockDim.x : 64, lane = WIDE ? (int)threadIdx.x : (int)threadIdx.x & 63;
   const S *X = (const S*)p.X, *dY = (const S*)p.dY;
   S* dX = (S*)p.dX;
-  P g[NV];
-  float ag[NV][VW], ab[NV][VW];
-#pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    g[i].fill(one_of<S>());
-#pragma unroll
-    for (int e = 0; e < VW; ++e) ag[i][e] = ab[i][e] = 0.f;
-  }
-  if (rows.task >= 0) {
-    const S* gp = (const S*)p.gamma[rows.task - p.task_base];
+  P g[NV], nx[NV], nd[NV];                               // weights; the next row
+  float nmean = 0.f, nrstd = 0.f;
+  auto load_next = [&](int r) {
+    const bool ok = r < rows.n && (rows.valid >> r & 1);
+    const int row = rows.row0 + r;
+    nmean = nrstd = 0.f;
+    if (ok) { nmean = p.mean[row]; nrstd = p.rstd[row]; }
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int c = (lane + i * LPR) * VW;
-      if (gp && c < p.N) g[i].load(gp + c);
+      const int c = (lane + i * lanes) * E;
+      nx[i].fill(0);
+      nd[i].fill(0);
+      if (ok && c < p.N) {
+        nx[i].template load<M == ODD ? ODD : WHOLE>(X + (size_t)row * p.ldx + c, p.N - c);
+        nd[i].template load<M == ODD ? ODD : WHOLE>(dY + (size_t)row * p.ldy + c, p.N - c);
+      }
+    }
+  };
+  load_next(WIDE ? 0 : wave);
+  float ag[NV][E], ab[NV][E];
+  {
+    const S* gp = (const S*)p.gamma[rows.range];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = (lane + i * lanes) * E;
+      g[i].fill(one_of<S>());
+      if (gp && c < p.N) g[i].template load<M == ODD ? ODD : WHOLE>(gp + c, p.N - c);
+#pragma unroll
+      for (int e = 0; e < E; ++e) ag[i][e] = ab[i][e] = 0.f;
     }
   }
   int slot = 0;
-  for (int r = rows.r0 + sub; r < rows.r1; r += SUBS) {
+  for (int r = WIDE ? 0 : wave; r < rows.n; r += STEP) {
+    const bool ok = rows.valid >> r & 1;
     const int row = rows.row0 + r;
-    S* dx = dX ? dX + (size_t)row * p.ldx : nullptr;
-    if (!(rows.valid >> r & 1)) {
-      if (!dx) continue;
-      const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        const int c = (lane + i * LPR) * VW;
-        if (c < p.N) P::store(dx + c, zero);
-      }
-      continue;
-    }
-    const S *x = X + (size_t)row * p.ldx, *dy = dY + (size_t)row * p.ldy;
     P xv[NV], dv[NV];
+    const float mean = nmean, rstd = nrstd;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int c = (lane + i * LPR) * VW;
-      xv[i].fill(0);
-      dv[i].fill(0);
-      if (c < p.N) { xv[i].load(x + c); dv[i].load(dy + c); }
-    }
-    const float mean = p.mean[row], rstd = p.rstd[row];
-    float s[2] = {0.f, 0.f};
+    for (int i = 0; i < NV; ++i) { xv[i] = nx[i]; dv[i] = nd[i]; }
+    load_next(r + STEP);
+    float s0 = 0.f, s1 = 0.f;
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
+    for (int i = 0; i < NV; ++i)                         // (dY = 0 past the row and on padding)
 #pragma unroll
-      for (int e = 0; e < VW; ++e) {
-        const float xh = (xv[i].get(e) - mean) * rstd, d = dv[i].get(e), h = d * g[i].get(e);   // (d = 0 past the row)
-        s[0] += h;
-        s[1] = fmaf(h, xh, s[1]);
+      for (int e = 0; e < E; ++e) {
+        const float xh = (xv[i].get(e) - mean) * rstd, d = dv[i].get(e), h = d * g[i].get(e);
+        s0 += h;
+        s1 = fmaf(h, xh, s1);
         ag[i][e] = fmaf(d, xh, ag[i][e]);
         ab[i][e] += d;
       }
-    if (dx) {                                          // (uniform: every lane of the grid takes the same way)
-      row_sum<LPR, 2>(s, lds, slot);
+    if (!dX) continue;                                   // (the same in every lane of the launch)
+    s0 = wave_sum(s0);
+    s1 = wave_sum(s1);
+    if constexpr (WIDE) {
+      const int waves = (int)blockDim.x >> 6;
+      if ((threadIdx.x & 63) == 0) part[slot][wave] = float2{s0, s1};
+      __syncthreads();
+      s0 = s1 = 0.f;
+      for (int w = 0; w < waves; ++w) { s0 += part[slot][w].x; s1 += part[slot][w].y; }
       slot ^= 1;
-      const float m1 = s[0] * p.inv_n, m2 = s[1] * p.inv_n;
+    }
+    const float m0 = s0 * p.inv_n, m1 = s1 * p.inv_n;
 #pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        const int c = (lane + i * LPR) * VW;
-        if (c >= p.N) continue;
-        float o[VW];
+    for (int i = 0; i < NV; ++i) {
+      const int c = (lane + i * lanes) * E;
+      if (c >= p.N) continue;
+      float o[E];
 #pragma unroll
-        for (int e = 0; e < VW; ++e) {
-          const float xh = (xv[i].get(e) - mean) * rstd, h = dv[i].get(e) * g[i].get(e);
-          o[e] = rstd * (h - m1 - xh * m2);
-        }
-        P::store(dx + c, o);
+      for (int e = 0; e < E; ++e) {
+        const float xh = (xv[i].get(e) - mean) * rstd, h = dv[i].get(e) * g[i].get(e);
+        o[e] = ok ? rstd * (h - m0 - xh * m1) : 0.f;
       }
+      P::template store<M>(dX + (size_t)row * p.ldx + c, o, p.N - c);
     }
   }
-  if (!p.part || !rows.any()) return;                  // (uniform in the workgroup; k_norm_reduce skips the same pieces)
-  float* part = p.part + ((size_t)p.item0 * (64 / p.rows) + blockIdx.x) * 2 * (size_t)p.N;
-  if constexpr (SUBS > 1) {
+  if (!p.part) return;
+  float* out = p.part + (size_t)blockIdx.x * 2 * (size_t)p.N;
+  if constexpr (!WIDE) {
     // the waves' sums one after the other, in a fixed order
-    for (int w = SUBS - 1; w >= 0; --w) {
-      if (sub == w) {
+    for (int w = 3; w >= 0; --w) {
+      if (wave == w) {
 #pragma unroll
         for (int i = 0; i < NV; ++i)
 #pragma unroll
-          for (int e = 0; e < VW; ++e) {
-            const int at = (i * VW + e) * LPR + lane;
-            if (w < SUBS - 1) { ag[i][e] += acc[0][at]; ab[i][e] += acc[1][at]; }
+          for (int e = 0; e < E; ++e) {
+            const int at = (i * E + e) * 64 + lane;
+            if (w < 3) { ag[i][e] += acc[0][at]; ab[i][e] += acc[1][at]; }
             if (w > 0) { acc[0][at] = ag[i][e]; acc[1][at] = ab[i][e]; }
           }
       }
       __syncthreads();
     }
-    if (sub != 0) return;
+    if (wave != 0) return;
   }
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    const int c = (lane + i * LPR) * VW;
-    if (c >= p.N) continue;
+    const int c = (lane + i * lanes) * E;
+    if (M != ODD && c >= p.N) continue;
 #pragma unroll
-    for (int e = 0; e < VW; ++e) { part[c + e] = ag[i][e]; part[p.N + c + e] = ab[i][e]; }
+    for (int q = 0; q < E; q += 4) {
+      Piece<float>::store<M == ODD ? ODD : WHOLE>(out + c + q, &ag[i][q], p.N - c - q);
+      Piece<float>::store<M == ODD ? ODD : WHOLE>(out + p.N + c + q, &ab[i][q], p.N - c - q);
+    }
   }
 }
 
 struct ReduceParams {
-  const int32_t* dtab;
   float* dgamma[kBatch];
   float* dbeta[kBatch];
-  int task_base, rows, N, accumulate;
-  const float* part;
+  int piece0[kBatch + 1];   // of the launch's tasks
+  int N, accumulate;
+  const float* part;        // null: a table without rows
 };
 
-// The pieces of a task added up, in their order inside a wave, the waves in order.  grid = (64 columns each, the tasks of the launch, 2: dgamma, dbeta)
+// The pieces of a task added up: a wave takes every sixteenth, in order, then the waves in order.  grid = (64 columns each, the
+// tasks of the launch, 2: dgamma, dbeta)
 __global__ __launch_bounds__(1024) void k_norm_reduce(ReduceParams p) {
   __shared__ float lds[16][64];
   const int t = blockIdx.y, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
@@ -313,17 +367,16 @@ __global__ __launch_bounds__(1024) void k_norm_reduce(ReduceParams p) {
   float* out = blockIdx.z ? p.dbeta[t] : p.dgamma[t];
   if (!out) return;
   float s = 0.f;
-  if (p.part) {                                          // (null: a table without rows)
-  const int32_t* ti = p.dtab + p.dtab[DH_NITEMS0 + 2] + 2 * (p.task_base + t);
-  const int per = 64 / p.rows, begin = ti[0] * per, end = begin + ti[1] * per;
-  const uint32_t* bits = (const uint32_t*)(p.dtab + p.dtab[DH_OFF_ITEM_BITS]);
-  const uint64_t ones = ~(uint64_t)0 >> (64 - p.rows);
-  for (int i = begin + wave; i < end; i += 16) {
-    const uint32_t* w = bits + 2 * (i / per);
-    const uint64_t valid = (uint64_t)w[0] | (uint64_t)w[1] << 32;
-    if ((valid >> (i % per * p.rows) & ones) == 0) continue;       // no token: nothing was written
-    if (c < p.N) s += p.part[((size_t)i * 2 + blockIdx.z) * (size_t)p.N + c];
-  }
+  if (p.part && c < p.N) {
+    const size_t step = 2 * (size_t)p.N;
+    const float* q = p.part + blockIdx.z * (size_t)p.N + c;
+    const int end = p.piece0[t + 1];
+    int i = p.piece0[t] + wave;
+    for (; i + 48 < end; i += 64) {                      // four loads on their way at a time
+      const float a0 = q[i * step], a1 = q[(i + 16) * step], a2 = q[(i + 32) * step], a3 = q[(i + 48) * step];
+      s += a0; s += a1; s += a2; s += a3;
+    }
+    for (; i < end; i += 16) s += q[i * step];
   }
   lds[wave][lane] = s;
   __syncthreads();
@@ -353,76 +406,102 @@ size_t extent(const mux_norm_desc* d, const mux_segtab* st, int64_t ld) {       
   return st->T > 0 ? ((size_t)(st->T - 1) * (size_t)ld + (size_t)d->width) * esize(d) : 0;
 }
 
-// Rows a workgroup takes, and so the number of partial sums.
-int piece_rows(const mux_segtab* st) {
-  int rows = 64;
-  while (rows > 4 && (st->T + rows - 1) / rows < 2 * kComputeUnits) rows /= 2;
-  return rows;
+int pieces_of(int rows, int per) { return (rows + per - 1) / per; }
+// 16-byte pieces of a row, the last one perhaps part of one
+int row_pieces(const mux_norm_desc* d) { return (int)(((size_t)d->width * esize(d) + 15) / 16); }
+
+// Rows a workgroup of the backward takes, and so the number of partial sums: enough workgroups for six waves a SIMD, twice what
+// stays there at a time, so that the last ones find their place (17637 x 5120, three, five, six, eight, ten: 140, 126, 124, 136, 135 us
+// and 8 to 15 for the sum of the pieces), of at least four rows.
+int piece_rows(const mux_norm_desc* d, const mux_segtab* st) {
+  const int n = row_pieces(d), waves = n <= 128 ? 4 : std::min(16, (n + 127) / 128);
+  return std::min(kMaxRows, std::max(4, pieces_of(st->T, std::max(1, 24 / waves) * kComputeUnits)));
+}
+int total_pieces(const mux_norm_desc* d, const mux_segtab* st) {
+  int n = 0, behind = 0;
+  const int rows = piece_rows(d, st);
+  for (const HostTask& t : st->tasks) {
+    n += pieces_of(t.row_count, rows);
+    behind = t.row_begin + t.row_count;
+  }
+  return n + pieces_of(st->T - behind, rows);            // (rows of no task lie behind the last one; their sums are zero)
 }
 
-#define NORM_CASE(K, S, VW, NV, LPR) \
-  else if (pieces <= NV * LPR) MUX_LAUNCH(name, (K<S, VW, NV, LPR>), grid, dim3(Rows<LPR>::THREADS), 0, stream, p)
-#define NORM_LAUNCH(K, wave_most)                                                                                      \
-  do {                                                                                                                 \
-    const int pieces = vec ? d->width * (int)esize(d) / 16 : d->width;                                                 \
-    if (d->dtype == MUX_DT_BF16 && vec) {                                                                              \
-      if (false) {}                                                                                                    \
-      NORM_CASE(K, bf16_t, 8, 1, 64); NORM_CASE(K, bf16_t, 8, 2, 64); NORM_CASE(K, bf16_t, 8, 4, 64);                  \
-      NORM_CASE(K, bf16_t, 8, 5, 64); NORM_CASE(K, bf16_t, 8, 8, 64); NORM_CASE(K, bf16_t, 8, 10, 64);                 \
-      NORM_CASE(K, bf16_t, 8, 4, 256); NORM_CASE(K, bf16_t, 8, 4, 1024);                                               \
-    } else if (d->dtype == MUX_DT_BF16) {                                                                              \
-      if (false) {}                                                                                                    \
-      NORM_CASE(K, bf16_t, 1, 8, 64); NORM_CASE(K, bf16_t, 1, 8, 256); NORM_CASE(K, bf16_t, 1, 20, 256);               \
-      NORM_CASE(K, bf16_t, 1, 32, 1024);                                                                               \
-    } else if (vec) {                                                                                                  \
-      if (false) {}                                                                                                    \
-      NORM_CASE(K, float, 4, 2, 64); NORM_CASE(K, float, 4, 4, 64); NORM_CASE(K, float, 4, 10, 64);                    \
-      NORM_CASE(K, float, 4, 16, 64); NORM_CASE(K, float, 4, 8, 256); NORM_CASE(K, float, 4, 8, 1024);                 \
-    } else {                                                                                                           \
-      if (false) {}                                                                                                    \
-      NORM_CASE(K, float, 1, 8, 64); NORM_CASE(K, float, 1, 8, 256); NORM_CASE(K, float, 1, 20, 256);                  \
-      NORM_CASE(K, float, 1, 32, 1024);                                                                                \
-    }                                                                                                                  \
-  } while (0)
-
-bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
-
-// Launches over the tasks of the table, kBatch at a time, each over the work items of its tasks (the first also over those
-// before them, the last over those behind).
+// A row of n pieces: one wave with NV of them a lane, or as many waves as it takes.
+#define NORM_CASE(K, S, NV, WAVES)                                                                                     \
+  if (n <= WAVES * 64 * NV) {                                                                                          \
+    const dim3 block(WAVES > 1 ? (unsigned)((n + 64 * NV - 1) / (64 * NV) * 64) : 256u);                                 \
+    if (mode == ODD) MUX_LAUNCH(name, (K<S, NV, WAVES, ODD>), grid, block, 0, stream, p);                               \
+    else if (mode == STREAM) MUX_LAUNCH(name, (K<S, NV, WAVES, STREAM>), grid, block, 0, stream, p);                    \
+    else MUX_LAUNCH(name, (K<S, NV, WAVES, WHOLE>), grid, block, 0, stream, p);                                        \
+    return;                                                                                                            \
+  }
 template <bool BACKWARD>
-void launch(const char* name, const mux_norm_desc* d, const mux_segtab* st, NormParams p, bool vec, hipStream_t stream) {
-  p.rows = piece_rows(st);
+void launch_one(const char* name, const mux_norm_desc* d, dim3 grid, const NormParams& p, Mode mode, hipStream_t stream) {
+  const int n = row_pieces(d);
+  if constexpr (BACKWARD) {
+    if (d->dtype == MUX_DT_BF16) {
+      NORM_CASE(k_norm_bwd, bf16_t, 1, 1) NORM_CASE(k_norm_bwd, bf16_t, 2, 1) NORM_CASE(k_norm_bwd, bf16_t, 2, 8)
+      NORM_CASE(k_norm_bwd, bf16_t, 4, 16)
+    } else {
+      NORM_CASE(k_norm_bwd, float, 1, 1) NORM_CASE(k_norm_bwd, float, 2, 1) NORM_CASE(k_norm_bwd, float, 2, 8)
+      NORM_CASE(k_norm_bwd, float, 4, 16) NORM_CASE(k_norm_bwd, float, 8, 16)
+    }
+  } else {
+    if (d->dtype == MUX_DT_BF16) {
+      NORM_CASE(k_norm_fwd, bf16_t, 1, 1) NORM_CASE(k_norm_fwd, bf16_t, 2, 1) NORM_CASE(k_norm_fwd, bf16_t, 4, 1)
+      NORM_CASE(k_norm_fwd, bf16_t, 6, 1) NORM_CASE(k_norm_fwd, bf16_t, 8, 1) NORM_CASE(k_norm_fwd, bf16_t, 10, 1)
+      NORM_CASE(k_norm_fwd, bf16_t, 2, 8) NORM_CASE(k_norm_fwd, bf16_t, 4, 16)
+    } else {
+      NORM_CASE(k_norm_fwd, float, 1, 1) NORM_CASE(k_norm_fwd, float, 2, 1) NORM_CASE(k_norm_fwd, float, 4, 1)
+      NORM_CASE(k_norm_fwd, float, 6, 1) NORM_CASE(k_norm_fwd, float, 8, 1) NORM_CASE(k_norm_fwd, float, 10, 1)
+      NORM_CASE(k_norm_fwd, float, 2, 8) NORM_CASE(k_norm_fwd, float, 4, 16) NORM_CASE(k_norm_fwd, float, 8, 16)
+    }
+  }
+}
+
+// Launches over the rows of the tasks, kBatch tasks at a time; the last also over the rows of no task.
+template <bool BACKWARD>
+void launch(const char* name, const mux_norm_desc* d, const mux_segtab* st, NormParams p, hipStream_t stream) {
+  p.in.rows = BACKWARD ? piece_rows(d, st) : 4;
+  const Mode mode = (size_t)d->width * esize(d) % 16 != 0 ? ODD : (size_t)st->T * (size_t)d->width * esize(d) > kStreamBytes ? STREAM : WHOLE;
+  float* const part = p.part;
+  int done = 0;                                          // pieces of the launches before
   for (int base = 0; base < st->n_tasks; base += kBatch) {
     const int n = std::min(kBatch, st->n_tasks - base);
-    p.task_base = base;
-    for (int i = 0; i < n; ++i) {
-      p.gamma[i] = d->gamma ? d->gamma[base + i] : nullptr;
-      p.beta[i] = d->beta ? d->beta[base + i] : nullptr;
+    int piece = 0, behind = 0;
+    p.in.n = 0;
+    for (int i = 0; i <= n; ++i) {
+      const bool none = i == n;                          // rows of no task lie behind the last one
+      if (none && base + n < st->n_tasks) break;
+      const HostTask* t = none ? nullptr : &st->tasks[base + i];
+      const int r0 = none ? behind : t->row_begin, r1 = none ? st->T : t->row_begin + t->row_count;
+      behind = r1;
+      if (r1 <= r0) continue;
+      const int k = p.in.n++;
+      p.gamma[k] = !none && d->gamma ? d->gamma[base + i] : nullptr;
+      p.beta[k] = !none && d->beta ? d->beta[base + i] : nullptr;
+      p.in.row0[k] = r0;
+      p.in.row1[k] = r1;
+      p.in.piece0[k] = piece;
+      piece += pieces_of(r1 - r0, p.in.rows);
     }
-    p.item0 = base == 0 ? 0 : st->task_item_begin[0][base];
-    const int end = base + n == st->n_tasks ? (int)st->items[0].size() : st->task_item_begin[0][base + n];
-    if (end <= p.item0) continue;
-    const dim3 grid((unsigned)(end - p.item0) * (unsigned)(64 / p.rows));
-    if constexpr (BACKWARD) NORM_LAUNCH(k_norm_bwd, 10);
-    else NORM_LAUNCH(k_norm_fwd, 10);
+    if (piece == 0) continue;
+    p.part = part ? part + (size_t)done * 2 * (size_t)p.N : nullptr;
+    launch_one<BACKWARD>(name, d, dim3((unsigned)piece), p, mode, stream);
+    done += piece;
   }
 }
 
-// Whether every row and weight can be moved in 16-byte pieces; false in `ok` where a pointer is not aligned to its element.
-bool pieces16(const mux_norm_desc* d, std::initializer_list<const void*> ptrs, bool& ok) {
-  const size_t e = esize(d);
-  bool vec = d->width * e % 16 == 0 && d->ldx * (int64_t)e % 16 == 0 && d->ldy * (int64_t)e % 16 == 0;
-  ok = true;
-  auto look = [&](const void* q) {
-    if ((uintptr_t)q % e) ok = false;
-    if (!aligned16(q)) vec = false;
-  };
-  for (const void* q : ptrs) look(q);
+// Whether every pointer is aligned to its element.
+bool aligned(const mux_norm_desc* d, std::initializer_list<const void*> ptrs) {
+  uintptr_t low = 0;
+  for (const void* q : ptrs) low |= (uintptr_t)q;
   for (int t = 0; t < d->n_tasks; ++t) {
-    if (d->gamma) look(d->gamma[t]);
-    if (d->beta) look(d->beta[t]);
+    if (d->gamma) low |= (uintptr_t)d->gamma[t];
+    if (d->beta) low |= (uintptr_t)d->beta[t];
   }
-  return vec;
+  return low % esize(d) == 0;
 }
 
 // Whether the bytes [w, w + nw) that a call writes overlap the [r, r + nr) that it reads in another way than row by row in place
@@ -447,8 +526,8 @@ extern "C" size_t mux_norm_saved_bytes(const mux_norm_desc* desc, const mux_segt
 }
 
 extern "C" size_t mux_norm_workspace_bytes(const mux_norm_desc* desc, const mux_segtab* st) {
-  if (!desc || !st || desc->width < 1) return 0;
-  return align256(st->items[0].size() * (size_t)(64 / piece_rows(st)) * 2 * (size_t)desc->width * sizeof(float));
+  if (!desc || !st || desc->width < 1 || desc->width > MUX_NORM_MAX_WIDTH) return 0;
+  return align256((size_t)total_pieces(desc, st) * 2 * (size_t)desc->width * sizeof(float));
 }
 
 extern "C" mux_status mux_norm_forward(const mux_norm_desc* desc, const mux_segtab* st, const void* dev_segtab, const void* X,
@@ -457,9 +536,7 @@ extern "C" mux_status mux_norm_forward(const mux_norm_desc* desc, const mux_segt
   if (mux_status s = check(fn, desc, st)) return s;
   if (st->T == 0) return MUX_OK;
   if (!dev_segtab || !X || !Y) return fail(MUX_ERR_INVALID_ARG, std::string(fn) + ": null device pointer");
-  bool ok;
-  const bool vec = pieces16(desc, {X, Y}, ok);
-  if (!ok || (uintptr_t)saved % 4) return fail(MUX_ERR_UNSUPPORTED, std::string(fn) + ": a pointer is not aligned to its element");
+  if (!aligned(desc, {X, Y}) || (uintptr_t)saved % 4) return fail(MUX_ERR_UNSUPPORTED, std::string(fn) + ": a pointer is not aligned to its element");
   const size_t nx = extent(desc, st, desc->ldx), ny = extent(desc, st, desc->ldy), nw = (size_t)desc->width * esize(desc);
   const size_t ns = (size_t)st->T * 2 * sizeof(float);
   bool bad = clash(Y, ny, desc->ldy, X, nx, desc->ldx) || overlap(saved, ns, X, nx) || overlap(saved, ns, Y, ny);
@@ -469,13 +546,13 @@ extern "C" mux_status mux_norm_forward(const mux_norm_desc* desc, const mux_segt
   }
   if (bad) return fail(MUX_ERR_INVALID_ARG, std::string(fn) + ": an output overlaps an input");
   NormParams p{};
-  p.dtab = (const int32_t*)dev_segtab;
+  p.rowbits = (const uint32_t*)dev_segtab + (dev_segtab ? st->dev_image[DH_OFF_ROWBITS] : 0);
   p.N = desc->width; p.T = st->T;
   p.eps = desc->eps; p.inv_n = 1.f / (float)desc->width;
   p.ldx = desc->ldx; p.ldy = desc->ldy;
   p.X = X; p.Y = Y;
   p.mean = (float*)saved; p.rstd = saved ? (float*)saved + st->T : nullptr;
-  launch<false>("norm_fwd", desc, st, p, vec, (hipStream_t)hip_stream);
+  launch<false>("norm_fwd", desc, st, p, (hipStream_t)hip_stream);
   return last_hip(fn);
 }
 
@@ -489,14 +566,14 @@ extern "C" mux_status mux_norm_backward(const mux_norm_desc* desc, const mux_seg
   const size_t nx = extent(desc, st, desc->ldx), ny = extent(desc, st, desc->ldy), nw = (size_t)desc->width * esize(desc);
   const size_t ng = (size_t)desc->width * sizeof(float), ns = (size_t)st->T * 2 * sizeof(float);
   std::vector<std::pair<uintptr_t, uintptr_t>> grads;    // the gradients' bytes
-  bool aligned = (uintptr_t)saved % 4 == 0;
+  bool floats = (uintptr_t)saved % 4 == 0;
   try {
     grads.reserve((size_t)desc->n_tasks * 2);
     for (int t = 0; t < desc->n_tasks; ++t)
       for (void* const* list : {dgamma, dbeta})
         if (list && list[t]) {
           grads.push_back({(uintptr_t)list[t], (uintptr_t)list[t] + ng});
-          aligned = aligned && (uintptr_t)list[t] % 4 == 0;
+          floats = floats && (uintptr_t)list[t] % 4 == 0;
         }
     std::sort(grads.begin(), grads.end());
   } catch (const std::bad_alloc&) {
@@ -507,9 +584,7 @@ extern "C" mux_status mux_norm_backward(const mux_norm_desc* desc, const mux_seg
   const size_t need = st->T > 0 && wants ? mux_norm_workspace_bytes(desc, st) : 0;
   if (need > 0 && !ws) return fail(MUX_ERR_INVALID_ARG, std::string(fn) + ": null workspace");
   if (ws_bytes < need) return fail(MUX_ERR_WORKSPACE, std::string(fn) + ": workspace too small");
-  bool ok;
-  const bool vec = pieces16(desc, {X, dY, dX}, ok);
-  if (!ok || !aligned || (need > 0 && (uintptr_t)ws % 4))
+  if (!aligned(desc, {X, dY, dX}) || !floats || (need > 0 && (uintptr_t)ws % 4))
     return fail(MUX_ERR_UNSUPPORTED, std::string(fn) + ": a pointer is not aligned to its element");
   bool bad = clash(dX, nx, desc->ldx, X, nx, desc->ldx) || clash(dX, nx, desc->ldx, dY, ny, desc->ldy) || overlap(dX, nx, saved, ns);
   for (size_t i = 0; i < grads.size(); ++i) {
@@ -523,28 +598,29 @@ extern "C" mux_status mux_norm_backward(const mux_norm_desc* desc, const mux_seg
   if (bad) return fail(MUX_ERR_INVALID_ARG, std::string(fn) + ": an output overlaps an input or another output");
   hipStream_t stream = (hipStream_t)hip_stream;
   NormParams p{};
-  p.dtab = (const int32_t*)dev_segtab;
+  p.rowbits = (const uint32_t*)dev_segtab + (dev_segtab ? st->dev_image[DH_OFF_ROWBITS] : 0);
   p.N = desc->width; p.T = st->T;
   p.eps = desc->eps; p.inv_n = 1.f / (float)desc->width;
   p.ldx = desc->ldx; p.ldy = desc->ldy;
   p.X = X; p.dY = dY; p.dX = dX;
   p.mean = (float*)saved; p.rstd = saved ? (float*)saved + st->T : nullptr;
   p.part = need > 0 ? (float*)ws : nullptr;
-  if (st->T > 0) launch<true>("norm_bwd", desc, st, p, vec, stream);
+  if (st->T > 0) launch<true>("norm_bwd", desc, st, p, stream);
   if (wants) {
     ReduceParams q{};
-    q.dtab = (const int32_t*)dev_segtab;
-    q.rows = piece_rows(st);
     q.N = desc->width;
     q.accumulate = accumulate;
     q.part = p.part;
+    int piece = 0;
     for (int base = 0; base < st->n_tasks; base += kBatch) {
       const int n = std::min(kBatch, st->n_tasks - base);
-      q.task_base = base;
       for (int i = 0; i < n; ++i) {
+        q.piece0[i] = piece;
+        piece += pieces_of(st->tasks[base + i].row_count, piece_rows(desc, st));
         q.dgamma[i] = dgamma ? (float*)dgamma[base + i] : nullptr;
         q.dbeta[i] = dbeta ? (float*)dbeta[base + i] : nullptr;
       }
+      q.piece0[n] = piece;
       MUX_LAUNCH("norm_reduce", k_norm_reduce, dim3((unsigned)(desc->width + 63) / 64, (unsigned)n, 2), dim3(1024), 0, stream, q);
     }
   }
