@@ -22,7 +22,7 @@ namespace {
 // device image of mux_pref_layout: a header of int32 words, then the sections whose word offsets it gives
 enum : int {
   PH_MAGIC = 0, PH_T, PH_NSEQS, PH_NPAIRS,
-  PH_OFF_ROW_SEQ,          // [T] sequence of the row, -1: padding
+  PH_OFF_ROW_SEQ,          // [T] sequence of the row, -1: padding (right behind the header)
   PH_OFF_SEQ,              // [n_seqs] first row, length
   PH_OFF_PAIR,             // [n_pairs] mux_pref_pair
   PH_OFF_PTR, PH_OFF_ENT,  // the pairs of sequence s: entries ptr[s] .. ptr[s + 1] - 1, each 2 * pair + (1: rejected)
@@ -30,7 +30,14 @@ enum : int {
 };
 constexpr int32_t kPrefMagic = 0x5250554D;
 constexpr int kThreads = 256;
-constexpr int kPieces = 4;                         // 16-byte pieces a thread holds of a slab
+// 16-byte pieces a thread holds of a slab.  Forward: a thread's loads are all on their way at once and its slabs few (8064 rows,
+// half of them counted, of 32000 bf16 entries: 4, 8, 16 pieces 48.5, 42.9, 46.7 us; 5120 rows of 128000: 240, 217, 227).
+// Backward: loads and stores of many workgroups mix better than those of few (1, 2, 3, 8 pieces: 128, 103, 126, 112; 470, 431, 472, 468).
+constexpr int kRowPieces = 8, kGradPieces = 2;
+// Up to so many (row, slab) parts one workgroup joins and sums them all and forms the losses (54 rows, one slab, one pair: 4.1 us for
+// 3.0 and 2.9 in two launches; 1920 rows, 4 slabs: 9.8 for 4.2).
+constexpr int kFewParts = 1024;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 constexpr float LOG2E = 1.4426950408889634f;
 
 template <class S> constexpr int per_piece() { return 16 / (int)sizeof(S); }
@@ -78,18 +85,19 @@ struct Slab {
 };
 
 __device__ __forceinline__ bool counted(const PrefParams& p, int row, int& seq, int& label) {
-  seq = p.layout[p.layout[PH_OFF_ROW_SEQ] + row];
+  seq = p.layout[PH_WORDS + row];
   label = p.labels[row];
   return seq >= 0 && label >= 0 && label < p.V;
 }
 
-// (maximum, sum) of two parts of a row
+// (maximum, sum) of two parts of a row; nothing but -inf in both leaves (-inf, 0)
 __device__ __forceinline__ void join(float& m, float& s, float m2, float s2) {
   const float top = fmaxf(m, m2), ref = top == -INFINITY ? 0.f : top;
   s = s * fast_exp(m - ref) + s2 * fast_exp(m2 - ref);
   m = top;
 }
 
+// 4032 counted rows of 32000 bf16 entries: 43 us, 6.0 TB/s (they were in part in the last-level cache); 5000 of 128000: 217 us, 5.9 TB/s.
 template <class S>
 __global__ __launch_bounds__(kThreads) void k_pref_rows(PrefParams p) {
   constexpr int E = per_piece<S>();
@@ -102,24 +110,25 @@ __global__ __launch_bounds__(kThreads) void k_pref_rows(PrefParams p) {
   const int tid = threadIdx.x;
   uint4 none;                                                    // pieces of -inf
   none.x = none.y = none.z = none.w = sizeof(S) == 2 ? 0xFF80FF80u : 0xFF800000u;
-  uint4 v[kPieces];
+  uint4 v[kRowPieces];
 #pragma unroll
-  for (int i = 0; i < kPieces; ++i) {
+  for (int i = 0; i < kRowPieces; ++i) {
     const int e = tid + i * kThreads;
-    v[i] = e < sl.n ? *(const uint4*)(x + sl.first + (size_t)e * E) : none;
+    v[i] = none;
+    if (e < sl.n) v[i] = *(const uint4*)(x + sl.first + (size_t)e * E);
   }
   float loose = -INFINITY;                                       // (one of at most 2 E - 2 elements outside the pieces)
   if (tid < sl.head) loose = Store<S>::ld(x, tid);
   else if (tid >= 64 && tid - 64 < sl.tails) loose = Store<S>::ld(x, sl.tail0 + tid - 64);
   float m = loose;
 #pragma unroll
-  for (int i = 0; i < kPieces; ++i)
+  for (int i = 0; i < kRowPieces; ++i)
 #pragma unroll
     for (int e = 0; e < E; ++e) m = fmaxf(m, elem(v[i], e, S()));
   const float ref = m == -INFINITY ? 0.f : m;
   float s = fast_exp(loose - ref);
 #pragma unroll
-  for (int i = 0; i < kPieces; ++i)
+  for (int i = 0; i < kRowPieces; ++i)
 #pragma unroll
     for (int e = 0; e < E; ++e) s += fast_exp(elem(v[i], e, S()) - ref);
 #pragma unroll
@@ -133,54 +142,33 @@ __global__ __launch_bounds__(kThreads) void k_pref_rows(PrefParams p) {
   }
 }
 
-// One workgroup a sequence: joins the slabs of its rows and sums the rows' log-probabilities.  Workgroups from n_seqs on
-// clear row_logp of the rows that belong to no sequence.
+// A row's log-probability (zero where it is not counted) from the parts of its slabs; also keeps what the backward needs.
 template <class S>
-__global__ __launch_bounds__(1024) void k_pref_seqs(PrefParams p) {
-  __shared__ double lds[16];
-  const int tid = threadIdx.x;
-  if ((int)blockIdx.x >= p.n_seqs) {
-    const int row = ((int)blockIdx.x - p.n_seqs) * 1024 + tid;
-    if (row < p.T && p.layout[p.layout[PH_OFF_ROW_SEQ] + row] < 0) p.row_logp[row] = 0.f;
-    return;
-  }
-  const int32_t* q = p.layout + p.layout[PH_OFF_SEQ] + 2 * (int)blockIdx.x;
-  const int first = q[0], len = q[1];
-  double sum = 0.0;
-  for (int r = tid; r < len; r += 1024) {
-    const int row = first + r, label = p.labels[row];
-    double lp = 0.0;
-    if (label >= 0 && label < p.V) {
-      const float x = Store<S>::ld((const S*)p.logits, (size_t)row * p.ld + label);
-      float2 a = p.part[(size_t)row * p.slabs];
-      for (int k = 1; k < p.slabs; ++k) {
-        const float2 b = p.part[(size_t)row * p.slabs + k];
-        join(a.x, a.y, b.x, b.y);
-      }
-      lp = (double)(x - a.x) - log((double)a.y);
-      if (p.stat) p.stat[row] = float2{a.x, 1.f / a.y};
+__device__ __forceinline__ double row_logp(const PrefParams& p, int row) {
+  const int label = p.labels[row];
+  double lp = 0.0;
+  if (label >= 0 && label < p.V) {
+    const float x = Store<S>::ld((const S*)p.logits, (size_t)row * p.ld + label);
+    float2 a = p.part[(size_t)row * p.slabs];
+    for (int k = 1; k < p.slabs; ++k) {
+      const float2 b = p.part[(size_t)row * p.slabs + k];
+      join(a.x, a.y, b.x, b.y);
     }
-    if (p.row_logp) p.row_logp[row] = (float)lp;
-    sum += lp;
+    lp = (double)(x - a.x) - log((double)a.y);
+    if (p.stat) p.stat[row] = float2{a.x, 1.f / a.y};
   }
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) sum += __shfl_xor(sum, o);
-  if ((tid & 63) == 0) lds[tid >> 6] = sum;
-  __syncthreads();
-  if (tid == 0) {
-    sum = 0.0;
-    for (int w = 0; w < 16; ++w) sum += lds[w];
-    p.seq_logp[blockIdx.x] = sum;
-    if (p.logp) p.logp[blockIdx.x] = (float)sum;
-  }
+  if (p.row_logp) p.row_logp[row] = (float)lp;
+  return lp;
 }
-
+__device__ __forceinline__ double wave_sum(double v) {
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o);
+  return v;
+}
 __device__ __forceinline__ double softplus(double z) { return fmax(z, 0.0) + log1p(exp(-fabs(z))); }
 __device__ __forceinline__ double sigmoid(double z) { return 1.0 / (1.0 + exp(-z)); }
 
-__global__ __launch_bounds__(256) void k_pref_pairs(PrefParams p) {
-  const int i = (int)blockIdx.x * 256 + (int)threadIdx.x;
-  if (i >= p.n_pairs) return;
+__device__ __forceinline__ void pair_loss(const PrefParams& p, int i) {
   const int32_t* q = p.layout + p.layout[PH_OFF_PAIR] + 4 * i;
   const int c = q[0], r = q[1];
   const double beta = __int_as_float(q[2]), e = __int_as_float(q[3]);
@@ -191,6 +179,59 @@ __global__ __launch_bounds__(256) void k_pref_pairs(PrefParams p) {
   if (e > 0.0) { loss += e * softplus(m); slope += e * sigmoid(m); }
   p.loss[i] = (float)loss;
   if (p.slope) p.slope[i] = (float)(beta * slope);
+}
+
+// Few rows: one workgroup does what k_pref_seqs and k_pref_pairs do, a wave a sequence at a time.
+template <class S>
+__global__ __launch_bounds__(1024) void k_pref_few(PrefParams p) {
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  if (p.row_logp)
+    for (int row = tid; row < p.T; row += 1024)
+      if (p.layout[PH_WORDS + row] < 0) p.row_logp[row] = 0.f;
+  const int32_t* seqs = p.layout + p.layout[PH_OFF_SEQ];
+  for (int s = wave; s < p.n_seqs; s += 16) {
+    const int first = seqs[2 * s], len = seqs[2 * s + 1];
+    double sum = 0.0;
+    for (int r = lane; r < len; r += 64) sum += row_logp<S>(p, first + r);
+    sum = wave_sum(sum);
+    if (lane == 0) {
+      p.seq_logp[s] = sum;
+      if (p.logp) p.logp[s] = (float)sum;
+    }
+  }
+  __syncthreads();                                               // (the workgroup's writes are there for its own reads)
+  for (int i = tid; i < p.n_pairs; i += 1024) pair_loss(p, i);
+}
+
+// One workgroup a sequence: sums its rows' log-probabilities.  Workgroups from n_seqs on clear row_logp of the rows that
+// belong to no sequence.
+template <class S>
+__global__ __launch_bounds__(1024) void k_pref_seqs(PrefParams p) {
+  __shared__ double lds[16];
+  const int tid = threadIdx.x;
+  if ((int)blockIdx.x >= p.n_seqs) {
+    const int row = ((int)blockIdx.x - p.n_seqs) * 1024 + tid;
+    if (row < p.T && p.layout[PH_WORDS + row] < 0) p.row_logp[row] = 0.f;
+    return;
+  }
+  const int32_t* q = p.layout + p.layout[PH_OFF_SEQ] + 2 * (int)blockIdx.x;
+  const int first = q[0], len = q[1];
+  double sum = 0.0;
+  for (int r = tid; r < len; r += 1024) sum += row_logp<S>(p, first + r);
+  sum = wave_sum(sum);
+  if ((tid & 63) == 0) lds[tid >> 6] = sum;
+  __syncthreads();
+  if (tid == 0) {
+    sum = 0.0;
+    for (int w = 0; w < 16; ++w) sum += lds[w];
+    p.seq_logp[blockIdx.x] = sum;
+    if (p.logp) p.logp[blockIdx.x] = (float)sum;
+  }
+}
+
+__global__ __launch_bounds__(256) void k_pref_pairs(PrefParams p) {
+  const int i = (int)blockIdx.x * 256 + (int)threadIdx.x;
+  if (i < p.n_pairs) pair_loss(p, i);
 }
 
 template <class S>
@@ -204,11 +245,19 @@ __device__ __forceinline__ uint4 pack<float>(const float* v) {
   return uint4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
 }
 
-// grid = (row, slab) as in k_pref_rows.  SAME: every row of dlogits begins at the same place inside 16 bytes as that of the logits.
-template <class S, bool SAME>
+// grid = (row, slab), the rows from the last to the first: those that the forward read last are still in the caches (124 us for
+// 128).  What is written goes past them where it is many (see kStreamBytes), so that they keep the logits (103 us; 431 us at 128000
+// entries, 6.0 TB/s of what is read and written).  SAME: every row of dlogits begins at the same place inside 16 bytes as that of the logits.
+template <bool STREAM>
+__device__ __forceinline__ void put(void* p, const uint4& v) {
+  if constexpr (STREAM) __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), (u32x4*)p);
+  else *(uint4*)p = v;
+}
+
+template <class S, bool SAME, bool STREAM>
 __global__ __launch_bounds__(kThreads) void k_pref_bwd(PrefParams p) {
   constexpr int E = per_piece<S>();
-  const int row = (int)(blockIdx.x / (unsigned)p.slabs), k = (int)(blockIdx.x % (unsigned)p.slabs);
+  const int row = p.T - 1 - (int)(blockIdx.x / (unsigned)p.slabs), k = (int)(blockIdx.x % (unsigned)p.slabs);
   const int tid = threadIdx.x;
   int seq, label;
   const bool on = counted(p, row, seq, label);
@@ -221,15 +270,15 @@ __global__ __launch_bounds__(kThreads) void k_pref_bwd(PrefParams p) {
   }
   if (e0 == e1) {                                                // not counted, or in no pair: zero, whatever the logits hold
     const Slab<S> sl(d, p.V, p.slab, k, p.slabs);
-    for (int e = tid; e < sl.n; e += kThreads) *(uint4*)(d + sl.first + (size_t)e * E) = uint4{0u, 0u, 0u, 0u};
+    for (int e = tid; e < sl.n; e += kThreads) put<STREAM>(d + sl.first + (size_t)e * E, uint4{0u, 0u, 0u, 0u});
     if (tid < sl.head) d[tid] = S(0);
     else if (tid >= 64 && tid - 64 < sl.tails) d[sl.tail0 + tid - 64] = S(0);
     return;
   }
   const Slab<S> sl(x, p.V, p.slab, k, p.slabs);
-  uint4 v[kPieces];
+  uint4 v[kGradPieces];
 #pragma unroll
-  for (int i = 0; i < kPieces; ++i) {
+  for (int i = 0; i < kGradPieces; ++i) {
     const int e = tid + i * kThreads;
     v[i] = uint4{0u, 0u, 0u, 0u};
     if (e < sl.n) v[i] = *(const uint4*)(x + sl.first + (size_t)e * E);
@@ -244,7 +293,7 @@ __global__ __launch_bounds__(kThreads) void k_pref_bwd(PrefParams p) {
   const float2 st = p.stat[row];
   const float f = -c * st.y;
 #pragma unroll
-  for (int i = 0; i < kPieces; ++i) {
+  for (int i = 0; i < kGradPieces; ++i) {
     const int e = tid + i * kThreads;
     if (e >= sl.n) continue;
     float o[E];
@@ -254,7 +303,7 @@ __global__ __launch_bounds__(kThreads) void k_pref_bwd(PrefParams p) {
       o[j] = f * fast_exp(elem(v[i], j, S()) - st.x);
       if (at + j == label) o[j] += c;
     }
-    if constexpr (SAME) *(uint4*)(d + at) = pack<S>(o);
+    if constexpr (SAME) put<STREAM>(d + at, pack<S>(o));
     else
 #pragma unroll
       for (int j = 0; j < E; ++j) Store<S>::st(d, (size_t)at + j, o[j]);
@@ -273,8 +322,8 @@ const int32_t* seq_words(const mux_segtab* st) {               // [task, pack, f
 size_t esize(const mux_pref_desc* d) { return d->dtype == MUX_DT_F32 ? 4 : 2; }
 
 // A row's slabs: as few as its elements need, of nearly the same size.
-void cut(const mux_pref_desc* d, int& slabs, int& slab) {
-  const int e = 16 / (int)esize(d), most = kThreads * kPieces * e;
+void cut(const mux_pref_desc* d, int pieces, int& slabs, int& slab) {
+  const int e = 16 / (int)esize(d), most = kThreads * pieces * e;
   slabs = (int)(((int64_t)d->vocab + most - 1) / most);
   slab = (int)((((int64_t)d->vocab + slabs - 1) / slabs + e - 1) / e * e);
 }
@@ -287,7 +336,7 @@ mux_status check(const char* fn, const mux_pref_desc* d, const mux_segtab* st, i
   const int64_t ld = grad ? std::max(d->ld, d->ldg) : d->ld;
   if (d->ld < d->vocab || (grad && d->ldg < d->vocab)) return fail(MUX_ERR_SHAPE, std::string(fn) + ": a leading dimension is smaller than the vocabulary");
   int slabs, slab;
-  cut(d, slabs, slab);
+  cut(d, std::min(kRowPieces, kGradPieces), slabs, slab);
   if (ld >= ((int64_t)1 << 40) || (int64_t)st->T * ld >= ((int64_t)1 << 42) || (int64_t)st->T * slabs >= ((int64_t)1 << 31) ||
       n_pairs > (1 << 28))
     return fail(MUX_ERR_SHAPE, std::string(fn) + ": problem too large");
@@ -371,7 +420,7 @@ extern "C" size_t mux_pref_saved_bytes(const mux_pref_desc* desc, const mux_segt
 extern "C" size_t mux_pref_workspace_bytes(const mux_pref_desc* desc, const mux_segtab* st) {
   if (!desc || !st || desc->vocab < 1) return 0;
   int slabs, slab;
-  cut(desc, slabs, slab);
+  cut(desc, kRowPieces, slabs, slab);
   return align256((size_t)n_seqs(st) * sizeof(double)) + align256((size_t)st->T * (size_t)slabs * sizeof(float2));
 }
 
@@ -402,7 +451,7 @@ extern "C" mux_status mux_pref_forward(const mux_pref_desc* desc, const mux_segt
   p.logits = logits; p.labels = labels; p.ref = ref_logp;
   p.row_logp = row_logp; p.logp = logp; p.loss = loss;
   p.T = st->T; p.V = desc->vocab; p.n_seqs = n_seqs(st); p.n_pairs = n_pairs;
-  cut(desc, p.slabs, p.slab);
+  cut(desc, kRowPieces, p.slabs, p.slab);
   p.seq_logp = (double*)ws;
   p.part = (float2*)((char*)ws + align256((size_t)p.n_seqs * sizeof(double)));
   if (saved) {
@@ -413,13 +462,16 @@ extern "C" mux_status mux_pref_forward(const mux_pref_desc* desc, const mux_segt
   const dim3 grid((unsigned)p.T * (unsigned)p.slabs);
   const unsigned clear = row_logp && st->valid_total < st->T ? (unsigned)((st->T + 1023) / 1024) : 0;
   const dim3 seqs((unsigned)p.n_seqs + clear);
-  if (desc->dtype == MUX_DT_F32) {
-    MUX_LAUNCH("pref_rows", k_pref_rows<float>, grid, dim3(kThreads), 0, stream, p);
-    MUX_LAUNCH("pref_seqs", k_pref_seqs<float>, seqs, dim3(1024), 0, stream, p);
-  } else {
-    MUX_LAUNCH("pref_rows", k_pref_rows<bf16_t>, grid, dim3(kThreads), 0, stream, p);
-    MUX_LAUNCH("pref_seqs", k_pref_seqs<bf16_t>, seqs, dim3(1024), 0, stream, p);
+  const bool f32 = desc->dtype == MUX_DT_F32;
+  if (f32) MUX_LAUNCH("pref_rows", k_pref_rows<float>, grid, dim3(kThreads), 0, stream, p);
+  else MUX_LAUNCH("pref_rows", k_pref_rows<bf16_t>, grid, dim3(kThreads), 0, stream, p);
+  if ((int64_t)st->T * p.slabs <= kFewParts) {
+    if (f32) MUX_LAUNCH("pref_few", k_pref_few<float>, dim3(1), dim3(1024), 0, stream, p);
+    else MUX_LAUNCH("pref_few", k_pref_few<bf16_t>, dim3(1), dim3(1024), 0, stream, p);
+    return last_hip(fn);
   }
+  if (f32) MUX_LAUNCH("pref_seqs", k_pref_seqs<float>, seqs, dim3(1024), 0, stream, p);
+  else MUX_LAUNCH("pref_seqs", k_pref_seqs<bf16_t>, seqs, dim3(1024), 0, stream, p);
   if (n_pairs > 0) MUX_LAUNCH("pref_pairs", k_pref_pairs, dim3((unsigned)(n_pairs + 255) / 256), dim3(256), 0, stream, p);
   return last_hip(fn);
 }
@@ -445,17 +497,18 @@ extern "C" mux_status mux_pref_backward(const mux_pref_desc* desc, const mux_seg
   p.logits = logits; p.labels = labels; p.dloss = dloss; p.dlogits = dlogits;
   p.T = st->T; p.V = desc->vocab; p.n_seqs = n_seqs(st); p.n_pairs = n_pairs;
   p.ld = desc->ld; p.ldg = desc->ldg;
-  cut(desc, p.slabs, p.slab);
+  cut(desc, kGradPieces, p.slabs, p.slab);
   p.stat = (float2*)saved;
   p.slope = (float*)((char*)saved + align256((size_t)st->T * sizeof(float2)));
   const bool same = (((uintptr_t)logits ^ (uintptr_t)dlogits) & 15) == 0 && ((desc->ld - desc->ldg) * (int64_t)e) % 16 == 0;
   const dim3 grid((unsigned)p.T * (unsigned)p.slabs);
-  if (desc->dtype == MUX_DT_F32) {
-    if (same) MUX_LAUNCH("pref_bwd", (k_pref_bwd<float, true>), grid, dim3(kThreads), 0, stream, p);
-    else MUX_LAUNCH("pref_bwd", (k_pref_bwd<float, false>), grid, dim3(kThreads), 0, stream, p);
-  } else {
-    if (same) MUX_LAUNCH("pref_bwd", (k_pref_bwd<bf16_t, true>), grid, dim3(kThreads), 0, stream, p);
-    else MUX_LAUNCH("pref_bwd", (k_pref_bwd<bf16_t, false>), grid, dim3(kThreads), 0, stream, p);
-  }
+  const bool past = (size_t)st->T * (size_t)desc->vocab * e > kStreamBytes;
+#define PREF_BWD(S, SAME)                                                                                            \
+  do {                                                                                                               \
+    if (past) MUX_LAUNCH("pref_bwd", (k_pref_bwd<S, SAME, true>), grid, dim3(kThreads), 0, stream, p);               \
+    else MUX_LAUNCH("pref_bwd", (k_pref_bwd<S, SAME, false>), grid, dim3(kThreads), 0, stream, p);                   \
+  } while (0)
+  if (desc->dtype == MUX_DT_F32) { if (same) PREF_BWD(float, true); else PREF_BWD(float, false); }
+  else { if (same) PREF_BWD(bf16_t, true); else PREF_BWD(bf16_t, false); }
   return last_hip(fn);
 }
