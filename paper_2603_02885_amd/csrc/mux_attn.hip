@@ -358,8 +358,10 @@ __global__ __launch_bounds__(256) void k_attn_zero_pad(ZeroParams p) {
   // wave w takes the rows w, w + 4, ..; the workgroup covers a slab of 256 vectors (4 KB) of the row width
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int slab = (int)blockIdx.y * 256 + lane;
+  const uint32_t* bits = (const uint32_t*)(p.dtab + p.dtab[DH_OFF_ITEM_BITS]) + 2 * blockIdx.x;
+  const uint64_t valid = (uint64_t)bits[0] | (uint64_t)bits[1] << 32;
   for (int r = wave; r < it.nrows; r += 4) {
-    if (it.task >= 0 && row_is_valid(p.dtab, it.row0 + r)) continue;
+    if (valid >> r & 1) continue;
     for (int o = 0; o < p.n_out; ++o) {
       uint4* dst = (uint4*)(p.out[o] + (size_t)(it.row0 + r) * p.ld[o]);
 #pragma unroll
@@ -543,9 +545,8 @@ __global__ __launch_bounds__(256, 1) void k_attn_sink_kv(AttnParams p) {
   work_item(p.n_blocks, p.Hkv * n_kt, wi_block, wi_head);
   const int kt = wi_head % n_kt;
   wi_head /= n_kt;
-  const int32_t* blk = p.dtab + p.list_off + (p.block0 + wi_block) * DA_WORDS;
+  const int32_t* blk = p.dtab + p.list_off + wi_block * DA_WORDS;
   const int first = blk[DA_FIRST_ROW], len = blk[DA_LEN], span0 = blk[DA_BLOCK0];
-  if (span0 % SINK_SPAN != 0) return;
   const int far = sink_far(p, len), qbegin = max(span0, far), qend = min(len, span0 + SINK_SPAN);
   if (qbegin >= qend) return;
   const int hc = wi_head * D, group = p.H / p.Hkv;
@@ -571,44 +572,49 @@ __global__ __launch_bounds__(256, 1) void k_attn_sink_kv(AttnParams p) {
   for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
     for (int j = 0; j < 16; ++j) { dk[dt][j] = 0.f; dv[dt][j] = 0.f; }
-  for (int g = 0; g < group; ++g) {
-    const int hq = wi_head * group + g, hcq = hq * D;
-    for (int qb = qbegin + QT * wave; qb < qend; qb += 4 * QT) {
-      TileLoadT<QT, D, 64> tq, td;
-      tq.load(p.Q, p.ldq, first, qb, qend, hcq, lane);
-      td.load(p.dO, p.ldo, first, qb, qend, hcq, lane);
-      float2 st = float2{INFINITY, 0.f};       // exp2(x - inf) = 0
-      if (li + qb < qend) {
-        const size_t at = (size_t)hq * p.T + first + qb + li;
-        st = float2{p.lse[at] * LOG2E, p.delta[at]};
-      }
-      wave_sync();
-      tq.store(sQ, TP, lane);
-      td.store(sD, TP, lane);
-      if (half == 0) stats[wave][li] = st;
-      wave_sync();
-      f32x16 s, dp;
+  // this wave's tiles of 32 queries, head after head of the group; the next one is on its way while one is computed
+  const int tiles_a_head = (qend - qbegin + 4 * QT - 1) / (4 * QT);
+  TileLoadT<QT, D, 64> tq, td;
+  float2 st;
+  auto load = [&](int i) {
+    const int hq = wi_head * group + i / tiles_a_head, qb = qbegin + QT * (wave + 4 * (i % tiles_a_head));
+    tq.load(p.Q, p.ldq, first, qb, qend, hq * D, lane);
+    td.load(p.dO, p.ldo, first, qb, qend, hq * D, lane);
+    st = float2{INFINITY, 0.f};                // exp2(x - inf) = 0
+    if (qb + li < qend) {
+      const size_t at = (size_t)hq * p.T + first + qb + li;
+      st = float2{p.lse[at] * LOG2E, p.delta[at]};
+    }
+  };
+  load(0);
+  for (int i = 0; i < group * tiles_a_head; ++i) {
+    wave_sync();
+    tq.store(sQ, TP, lane);
+    td.store(sD, TP, lane);
+    if (half == 0) stats[wave][li] = st;
+    wave_sync();
+    if (i + 1 < group * tiles_a_head) load(i + 1);
+    f32x16 s, dp;
 #pragma unroll
-      for (int j = 0; j < 16; ++j) { s[j] = 0.f; dp[j] = 0.f; }
+    for (int j = 0; j < 16; ++j) { s[j] = 0.f; dp[j] = 0.f; }
 #pragma unroll
-      for (int k = 0; k < KS; ++k) {
-        s = mma(*(const bf16x8*)(sQ + li * TP + 16 * k + 8 * half), kf[k], s);
-        dp = mma(*(const bf16x8*)(sD + li * TP + 16 * k + 8 * half), vf[k], dp);
-      }
+    for (int k = 0; k < KS; ++k) {
+      s = mma(*(const bf16x8*)(sQ + li * TP + 16 * k + 8 * half), kf[k], s);
+      dp = mma(*(const bf16x8*)(sD + li * TP + 16 * k + 8 * half), vf[k], dp);
+    }
 #pragma unroll
-      for (int j = 0; j < 16; ++j) {           // every query here lies behind the keys: no mask (lanes past n_sinks are not stored)
-        const float2 q = stats[wave][tok(j, half)];
-        s[j] = fast_exp2(fmaf(s[j], c, -q.x));
-        dp[j] = s[j] * (dp[j] - q.y);
-      }
+    for (int j = 0; j < 16; ++j) {           // every query here lies behind the keys: no mask (lanes past n_sinks are not stored)
+      const float2 q = stats[wave][tok(j, half)];
+      s[j] = fast_exp2(fmaf(s[j], c, -q.x));
+      dp[j] = s[j] * (dp[j] - q.y);
+    }
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const bf16x8 pb = pack8(s, u), ds = pack8(dp, u);
+    for (int u = 0; u < 2; ++u) {
+      const bf16x8 pb = pack8(s, u), ds = pack8(dp, u);
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt) {
-          dv[dt] = mma(read_across<TP>(sD, 16 * u, 32 * dt, lane), pb, dv[dt]);
-          dk[dt] = mma(read_across<TP>(sQ, 16 * u, 32 * dt, lane), ds, dk[dt]);
-        }
+      for (int dt = 0; dt < DT; ++dt) {
+        dv[dt] = mma(read_across<TP>(sD, 16 * u, 32 * dt, lane), pb, dv[dt]);
+        dk[dt] = mma(read_across<TP>(sQ, 16 * u, 32 * dt, lane), ds, dk[dt]);
       }
     }
   }
@@ -630,7 +636,7 @@ __global__ __launch_bounds__(256, 1) void k_attn_sink_kv(AttnParams p) {
     __syncthreads();
   }
   if (wave == 0 && kl < p.n_sinks) {
-    float* part = p.sinks + sink_part<D>(p, blk[DA_SINK_SLOT] + span0 / SINK_SPAN, wi_head) + (size_t)kl * D + 4 * half;
+    float* part = p.sinks + sink_part<D>(p, blk[DA_SINK_SLOT], wi_head) + (size_t)kl * D + 4 * half;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
@@ -1219,9 +1225,13 @@ mux_status backward(const char* fn, const mux_attn_desc* desc, Window w, const m
     p.n_blocks = n_long;
     ATTN_LAUNCH("attn_delta", k_attn_delta, D, dim3((unsigned)(((n + 3) / 4 * 16 + 255) / 256)), stream, p);
     if (sink_bytes(desc, st, w) > 0) {
+      AttnParams q = p;
+      q.n_blocks = st->n_attn_spans;
+      q.list_off = st->dev_image[DH_ATT_OFF_SPANS];
       if ((uintptr_t)ws % 16) return fail(MUX_ERR_UNSUPPORTED, std::string(fn) + ": the workspace must be 16-byte aligned");
       p.sinks = (float*)((char*)ws + mux_attn_workspace_bytes(desc, st));
-      ATTN_LAUNCH("attn_sink_kv", k_attn_sink_kv, D, dim3((unsigned)n_long * (unsigned)(desc->n_kv_heads * ((w.n_sinks + 31) / 32))), stream, p);
+      q.sinks = p.sinks;
+      ATTN_LAUNCH("attn_sink_kv", k_attn_sink_kv, D, dim3((unsigned)q.n_blocks * (unsigned)(desc->n_kv_heads * ((w.n_sinks + 31) / 32))), stream, q);
     }
     ATTN_LAUNCH_WIN("attn_bwd_kv", k_attn_bwd_kv, D, win, dim3((unsigned)n_long * (unsigned)desc->n_kv_heads), stream, p);
     AttnParams q = p;

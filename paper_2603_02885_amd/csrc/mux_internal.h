@@ -24,6 +24,7 @@ enum : int {
   DH_OFF_GEMM_ITEMS,     // the 256-row work items ordered for the backbone product (see mux_segtab::n_gemm), DI_WORDS each,
                          // with the rows up to the last real token in the place of DI_NVALID
   DH_OFF_GEMM_ITEMS64,   // the same of the 64-row work items (see mux_segtab::n_gemm64)
+  DH_ATT_OFF_SPANS,      // the sequences' spans of kAttnSinkSpan blocks, 4 words an entry (DA_*), its own number in the last
   DH_HDR_WORDS = 32
 };
 constexpr int kNumTileSizes = 4;
@@ -32,8 +33,8 @@ constexpr uint32_t kDevMagic = 0x4458554Du;  // "MUXD"
 
 // per task, 8 words
 enum : int { DT_ROW_BEGIN = 0, DT_ROW_COUNT, DT_VALID, DT_KIND, DT_RANK, DT_SCALE_BITS, DT_ZROW0, DT_ITEM_PAD, DT_WORDS };
-// per attention block, 4 words: the sequence's first row and length, the block's first token inside the sequence, and in the
-// second list the number of the sequence's first span of kAttnSinkSpan blocks, counted through the sequences
+// per attention block or span, 4 words: the sequence's first row and length, the block's first token inside the sequence, and in the
+// second list of blocks and that of spans the number of the sequence's first or the span's own place among the spans
 enum : int { DA_FIRST_ROW = 0, DA_LEN, DA_BLOCK0, DA_SINK_SLOT, DA_WORDS };
 constexpr int kAttnBlockRows = 128, kAttnSinkSpan = 4;
 // per work item, 4 words: rows [row0, row0+nrows) all belong to `task` (-1: rows of no task)

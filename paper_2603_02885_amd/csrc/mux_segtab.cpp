@@ -290,12 +290,12 @@ extern "C" mux_status mux_segtab_build(const mux_task_desc* tasks, int32_t n_tas
       struct Blk { int32_t first_row, len, b0, slot; };
       std::vector<Seq> order(seqs.begin(), seqs.end());
       std::stable_sort(order.begin(), order.end(), [](const Seq& a, const Seq& b) { return a.len > b.len; });
-      std::vector<Blk> fwd, bwd;
+      std::vector<Blk> fwd, bwd, spans;
       for (const Seq& sq : order) {
         const int32_t nb = (sq.len + kAttnBlockRows - 1) / kAttnBlockRows;
         for (int32_t b = nb - 1; b >= 0; --b) fwd.push_back({sq.first_row, sq.len, b * kAttnBlockRows, 0});
         for (int32_t b = 0; b < nb; ++b) bwd.push_back({sq.first_row, sq.len, b * kAttnBlockRows, st->n_attn_spans});
-        st->n_attn_spans += (nb + kAttnSinkSpan - 1) / kAttnSinkSpan;
+        for (int32_t b = 0; b < nb; b += kAttnSinkSpan) spans.push_back({sq.first_row, sq.len, b * kAttnBlockRows, st->n_attn_spans++});
         if (sq.len <= kAttnBlockRows / 2) st->n_attn_blocks64 += nb;
         else if (sq.len <= kAttnBlockRows) st->n_attn_blocks128 += nb;
       }
@@ -304,6 +304,8 @@ extern "C" mux_status mux_segtab_build(const mux_task_desc* tasks, int32_t n_tas
       dv[DH_ATT_NBLK] = st->n_attn_blocks;
       dv[DH_ATT_OFF_FWD] = (int32_t)dv.size();
       for (const Blk& b : fwd) { const int32_t w[DA_WORDS] = {b.first_row, b.len, b.b0, b.slot}; dv.insert(dv.end(), w, w + DA_WORDS); }
+      dv[DH_ATT_OFF_SPANS] = (int32_t)dv.size();
+      for (const Blk& b : spans) { const int32_t w[DA_WORDS] = {b.first_row, b.len, b.b0, b.slot}; dv.insert(dv.end(), w, w + DA_WORDS); }
       dv[DH_ATT_OFF_BWD] = (int32_t)dv.size();
       for (const Blk& b : bwd) { const int32_t w[DA_WORDS] = {b.first_row, b.len, b.b0, b.slot}; dv.insert(dv.end(), w, w + DA_WORDS); }
     }
