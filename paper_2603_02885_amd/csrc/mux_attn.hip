@@ -12,6 +12,8 @@
 // ds_read_b64_tr_b16.  A sum over 16 tokens may take them in any order as long as both operands agree; the order
 // used is the one the accumulator layout gives: slot i of half-wave h <-> token 8 (i / 4) + 4 h + i % 4.
 // Every output element has one owner; nothing is accumulated across workgroups, results repeat bit for bit.
+#include <type_traits>
+
 #include "mux_attn.h"
 #include "mux_device_utils.h"
 
@@ -21,6 +23,7 @@ namespace {
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
 typedef __attribute__((ext_vector_type(16))) float f32x16;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 
 constexpr int BLK = kAttnBlockRows;
 constexpr int TILE = 64;        // tokens of the other side staged per step
@@ -59,7 +62,7 @@ struct AttnParams {
 };
 // Whether a query sees the key `ahead` tokens before it
 __device__ __forceinline__ bool in_window(const AttnParams& p, int ahead, bool sink) {
-  return (unsigned)ahead < (unsigned)p.window || (sink && ahead >= 0);
+  return (int)((unsigned)ahead < (unsigned)p.window) | ((int)sink & (int)(ahead >= 0));
 }
 
 __device__ __forceinline__ bf16x4 lds_read_tr(const bf16_t* p) {
@@ -176,6 +179,37 @@ struct TileLoadT {
     }
   }
 };
+// The same for the WIN kernels: the NTHR threads take the pieces in order, so that an instruction reads whole rows side by side, and
+// rows from `rows` on are the last one again instead of zero (finite; their keys and queries are masked, their probabilities
+// zero), so that no lane is switched off and an address is a scalar plus 32 bits.  `tile`: the head's columns of the tile's first
+// row, the same in every lane.
+template <int ROWS, int D, int NTHR = 256>
+struct RowsInTurn {
+  static constexpr int PPR = D / 8, NP = ROWS * PPR, N = (NP + NTHR - 1) / NTHR;
+  u32x4 r[N];
+  __device__ __forceinline__ void load(const bf16_t* tile, uint32_t ld, int rows, int tid) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int e = tid + NTHR * i, row = min(e / PPR, rows - 1);
+      r[i] = *(const u32x4*)((const char*)tile + ((uint32_t)row * ld + (uint32_t)(e % PPR * 8)) * 2u);
+    }
+  }
+  __device__ __forceinline__ void store(bf16_t* tile, int pitch, int tid) const {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int e = tid + NTHR * i;
+      if (NP % NTHR == 0 || e < NP) *(u32x4*)(tile + e / PPR * pitch + e % PPR * 8) = r[i];
+    }
+  }
+};
+template <bool WIN, int ROWS, int D, int NTHR = 256>
+using TileLoad = std::conditional_t<WIN, RowsInTurn<ROWS, D, NTHR>, TileLoadT<ROWS, D, NTHR>>;
+// Rows row0 .. of one head's columns, of a sequence of `len` rows from `first` on
+template <class L>
+__device__ __forceinline__ void load_rows(L& t, const bf16_t* base, int64_t ld, int first, int row0, int len, int hc, int tid) {
+  if constexpr (std::is_same_v<decltype(t.r[0]), u32x4&>) t.load(base + (size_t)(first + row0) * ld + hc, (uint32_t)ld, len - row0, tid);
+  else t.load(base, ld, first, row0, len, hc, tid);
+}
 // Zero in the columns D .. DP-1 of a staged tile of `rows` rows (nothing is ever stored there afterwards).
 template <int D, int DP, int NTHR = 256>
 __device__ __forceinline__ void zero_pad_columns(bf16_t* tile, int rows, int pitch, int tid) {
@@ -222,11 +256,11 @@ __global__ __launch_bounds__(256, 2) void k_attn_fwd(AttnParams p) {
   const float lazy = 8.f / c;                   // 8 in the exponent, in units of the raw score
   const int kend = min(len, q0 + BLK);          // keys [0, kend) are visible to some query of the block
   const int wq_first = q0 + 32 * wave, wq_last = wq_first + 31;
-  TileLoadT<TILE, D> tk, tv;
+  TileLoad<WIN, TILE, D> tk, tv;
   const int hck = wi_head / (p.H / p.Hkv) * D;  // this head's key/value columns
   const int kwin = WIN ? window_tile(p, q0) : 0, kfirst = WIN && p.n_sinks == 0 ? kwin : 0;
-  tk.load(p.K, p.ldk, first, kfirst, len, hck, tid);
-  tv.load(p.V, p.ldv, first, kfirst, len, hck, tid);
+  load_rows(tk, p.K, p.ldk, first, kfirst, len, hck, tid);
+  load_rows(tv, p.V, p.ldv, first, kfirst, len, hck, tid);
   for (int kb = kfirst, kn; kb < kend; kb = kn) {
     kn = kb + TILE;
     if (WIN && kn < kwin) kn = kwin;
@@ -235,8 +269,8 @@ __global__ __launch_bounds__(256, 2) void k_attn_fwd(AttnParams p) {
     tv.store(sV, TP, tid);
     __syncthreads();
     if (kn < kend) {
-      tk.load(p.K, p.ldk, first, kn, len, hck, tid);
-      tv.load(p.V, p.ldv, first, kn, len, hck, tid);
+      load_rows(tk, p.K, p.ldk, first, kn, len, hck, tid);
+      load_rows(tv, p.V, p.ldv, first, kn, len, hck, tid);
     }
     if (kb > wq_last) continue;                 // no key of this tile is visible to this wave's queries
     if (WIN && kb + TILE <= wq_first - p.window + 1 && kb >= p.n_sinks) continue;
@@ -446,11 +480,11 @@ __global__ __launch_bounds__(256, 2) void k_attn_bwd_q(AttnParams p) {
     for (int j = 0; j < 16; ++j) dq[dt][j] = 0.f;
   const int kend = min(len, q0 + BLK);
   const int wq_first = q0 + 32 * wave, wq_last = wq_first + 31;
-  TileLoadT<TILE, D> tk, tv;
+  TileLoad<WIN, TILE, D> tk, tv;
   const int hck = wi_head / (p.H / p.Hkv) * D;  // this head's key/value columns
   const int kwin = WIN ? window_tile(p, q0) : 0, kfirst = WIN && p.n_sinks == 0 ? kwin : 0;
-  tk.load(p.K, p.ldk, first, kfirst, len, hck, tid);
-  tv.load(p.V, p.ldv, first, kfirst, len, hck, tid);
+  load_rows(tk, p.K, p.ldk, first, kfirst, len, hck, tid);
+  load_rows(tv, p.V, p.ldv, first, kfirst, len, hck, tid);
   for (int kb = kfirst, kn; kb < kend; kb = kn) {
     kn = kb + TILE;
     if (WIN && kn < kwin) kn = kwin;
@@ -459,8 +493,8 @@ __global__ __launch_bounds__(256, 2) void k_attn_bwd_q(AttnParams p) {
     tv.store(sV, KP, tid);
     __syncthreads();
     if (kn < kend) {
-      tk.load(p.K, p.ldk, first, kn, len, hck, tid);
-      tv.load(p.V, p.ldv, first, kn, len, hck, tid);
+      load_rows(tk, p.K, p.ldk, first, kn, len, hck, tid);
+      load_rows(tv, p.V, p.ldv, first, kn, len, hck, tid);
     }
     if (kb > wq_last) continue;
     if (WIN && kb + TILE <= wq_first - p.window + 1 && kb >= p.n_sinks) continue;
@@ -535,7 +569,7 @@ __device__ __forceinline__ size_t sink_part(const AttnParams& p, int slot, int h
   return ((size_t)slot * p.Hkv + head) * (size_t)p.n_sinks * (2 * D);
 }
 template <int D>
-__global__ __launch_bounds__(256, 1) void k_attn_sink_kv(AttnParams p) {
+__global__ __launch_bounds__(256, 2) void k_attn_sink_kv(AttnParams p) {
   constexpr int KS = Dim<D>::KS, DT = Dim<D>::DT, DP = Dim<D>::DP, TP = Dim<D>::TP, QT = SINK_TILE;
   __shared__ __align__(16) bf16_t tiles[4][2][QT * TP];
   __shared__ float2 stats[4][QT];
@@ -574,26 +608,26 @@ __global__ __launch_bounds__(256, 1) void k_attn_sink_kv(AttnParams p) {
     for (int j = 0; j < 16; ++j) { dk[dt][j] = 0.f; dv[dt][j] = 0.f; }
   // this wave's tiles of 32 queries, head after head of the group; the next one is on its way while one is computed
   const int tiles_a_head = (qend - qbegin + 4 * QT - 1) / (4 * QT);
-  TileLoadT<QT, D, 64> tq, td;
+  RowsInTurn<QT, D, 64> tq, td;
   float2 st;
   auto load = [&](int i) {
     const int hq = wi_head * group + i / tiles_a_head, qb = qbegin + QT * (wave + 4 * (i % tiles_a_head));
-    tq.load(p.Q, p.ldq, first, qb, qend, hq * D, lane);
-    td.load(p.dO, p.ldo, first, qb, qend, hq * D, lane);
+    const int at = min(qb, qend - 1);          // (a wave without rows of its own in the last turn computes on that one, to no effect)
+    load_rows(tq, p.Q, p.ldq, first, at, qend, hq * D, lane);
+    load_rows(td, p.dO, p.ldo, first, at, qend, hq * D, lane);
     st = float2{INFINITY, 0.f};                // exp2(x - inf) = 0
     if (qb + li < qend) {
       const size_t at = (size_t)hq * p.T + first + qb + li;
       st = float2{p.lse[at] * LOG2E, p.delta[at]};
     }
   };
-  load(0);
   for (int i = 0; i < group * tiles_a_head; ++i) {
+    load(i);
     wave_sync();
     tq.store(sQ, TP, lane);
     td.store(sD, TP, lane);
     if (half == 0) stats[wave][li] = st;
     wave_sync();
-    if (i + 1 < group * tiles_a_head) load(i + 1);
     f32x16 s, dp;
 #pragma unroll
     for (int j = 0; j < 16; ++j) { s[j] = 0.f; dp[j] = 0.f; }
@@ -601,6 +635,7 @@ __global__ __launch_bounds__(256, 1) void k_attn_sink_kv(AttnParams p) {
     for (int k = 0; k < KS; ++k) {
       s = mma(*(const bf16x8*)(sQ + li * TP + 16 * k + 8 * half), kf[k], s);
       dp = mma(*(const bf16x8*)(sD + li * TP + 16 * k + 8 * half), vf[k], dp);
+      if (k % 2 == 1) __builtin_amdgcn_sched_barrier(0);       // (as in k_attn_bwd_kv: the operand reads would pile up in registers)
     }
 #pragma unroll
     for (int j = 0; j < 16; ++j) {           // every query here lies behind the keys: no mask (lanes past n_sinks are not stored)
@@ -616,6 +651,7 @@ __global__ __launch_bounds__(256, 1) void k_attn_sink_kv(AttnParams p) {
         dv[dt] = mma(read_across<TP>(sD, 16 * u, 32 * dt, lane), pb, dv[dt]);
         dk[dt] = mma(read_across<TP>(sQ, 16 * u, 32 * dt, lane), ds, dk[dt]);
       }
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
   // the waves' sums, last wave first; a lane's column of 16 dt values lies 64 lanes apart (no bank twice)
@@ -689,7 +725,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_bwd_kv(AttnParams p) {
 #pragma unroll
     for (int j = 0; j < 16; ++j) { dk[dt][j] = 0.f; dv[dt][j] = 0.f; }
   const int wk_first = k0 + 32 * wave;
-  TileLoadT<QT, D> tq, td;
+  TileLoad<WIN, QT, D> tq, td;
   float r_lse = 0.f, r_delta = 0.f;
   for (int g = 0; g < group; ++g) {             // every query head that reads this key/value head
   const int hq = wi_head * group + g, hcq = hq * D;
@@ -700,8 +736,8 @@ __global__ __launch_bounds__(256, 2) void k_attn_bwd_kv(AttnParams p) {
       r_delta = ok ? p.delta[(size_t)hq * p.T + first + qb + tid] : 0.f;
     }
   };
-  tq.load(p.Q, p.ldq, first, k0, len, hcq, tid);
-  td.load(p.dO, p.ldo, first, k0, len, hcq, tid);
+  load_rows(tq, p.Q, p.ldq, first, k0, len, hcq, tid);
+  load_rows(td, p.dO, p.ldo, first, k0, len, hcq, tid);
   load_stats(k0);
   const int qend = WIN ? min(len, k0 + BLK - 1 + p.window) : len;
   for (int qb = k0; qb < qend; qb += QT) {      // queries before the block see none of its keys
@@ -711,8 +747,8 @@ __global__ __launch_bounds__(256, 2) void k_attn_bwd_kv(AttnParams p) {
     if (tid < QT) { sLse[tid] = r_lse; sDelta[tid] = r_delta; }
     __syncthreads();
     if (qb + QT < qend) {
-      tq.load(p.Q, p.ldq, first, qb + QT, len, hcq, tid);
-      td.load(p.dO, p.ldo, first, qb + QT, len, hcq, tid);
+      load_rows(tq, p.Q, p.ldq, first, qb + QT, len, hcq, tid);
+      load_rows(td, p.dO, p.ldo, first, qb + QT, len, hcq, tid);
       load_stats(qb + QT);
     }
     if (qb + QT - 1 < wk_first) continue;     // every query of the tile lies before this wave's keys
@@ -1142,6 +1178,13 @@ mux_status check_window(const char* fn, int32_t window, int32_t n_sinks) {
   if (n_sinks > MUX_ATTN_MAX_SINKS) return fail(MUX_ERR_UNSUPPORTED, std::string(fn) + ": n_sinks above MUX_ATTN_MAX_SINKS");
   return MUX_OK;
 }
+// (the WIN kernels' lanes reach the rows of a tile with 32 bits)
+mux_status check_rows(const char* fn, const mux_attn_desc* d, Window w) {
+  const int64_t most = (int64_t)1 << 24;
+  if (w.window > 0 && (d->ldq >= most || d->ldk >= most || d->ldv >= most || d->ldo >= most))
+    return fail(MUX_ERR_SHAPE, std::string(fn) + ": a leading dimension of 2^24 elements or more");
+  return MUX_OK;
+}
 // A window that no sequence is longer than hides nothing.
 Window effective(const mux_segtab* st, int32_t window, int32_t n_sinks) {
   return st && window < st->attn_longest ? Window{window, n_sinks} : Window{0, 0};
@@ -1150,6 +1193,7 @@ Window effective(const mux_segtab* st, int32_t window, int32_t n_sinks) {
 mux_status forward(const char* fn, const mux_attn_desc* desc, Window w, const mux_segtab* st, const void* dev_segtab, const void* Q,
                    const void* K, const void* V, void* O, void* saved, void* hip_stream) {
   if (mux_status s = check(fn, desc, st)) return s;
+  if (mux_status s = check_rows(fn, desc, w)) return s;
   if (st->T == 0) return MUX_OK;
   if (!dev_segtab || !Q || !K || !V || !O) return fail(MUX_ERR_INVALID_ARG, std::string(fn) + ": null device pointer");
   if (!aligned16(Q) || !aligned16(K) || !aligned16(V) || !aligned16(O))
@@ -1192,6 +1236,7 @@ mux_status backward(const char* fn, const mux_attn_desc* desc, Window w, const m
                     const void* K, const void* V, const void* O, const void* dO, const void* saved, void* dQ, void* dK, void* dV,
                     void* ws, size_t ws_bytes, void* hip_stream) {
   if (mux_status s = check(fn, desc, st)) return s;
+  if (mux_status s = check_rows(fn, desc, w)) return s;
   if (st->T == 0) return MUX_OK;
   if (!dev_segtab || !Q || !K || !V || !O || !dO || !saved || !dQ || !dK || !dV || !ws)
     return fail(MUX_ERR_INVALID_ARG, std::string(fn) + ": null device pointer");
