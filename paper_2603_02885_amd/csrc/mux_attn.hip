@@ -706,16 +706,34 @@ __global__ __launch_bounds__(256, 2) void k_attn_bwd_kv(AttnParams p) {
   const bool kok = kl < len;
   zero_pad_columns<D, DP>(sQ, QT, TP, tid);
   zero_pad_columns<D, DP>(sD, QT, TP, tid);
+  TileLoad<WIN, QT, D> tq, td;
+  float r_lse = 0.f, r_delta = 0.f;
+  auto load_stats = [&](int hq, int qb) {
+    if (tid < QT) {
+      const bool ok = qb + tid < len;
+      r_lse = ok ? p.lse[(size_t)hq * p.T + first + qb + tid] * LOG2E : INFINITY;   // exp2(x - inf) = 0
+      r_delta = ok ? p.delta[(size_t)hq * p.T + first + qb + tid] : 0.f;
+    }
+  };
   bf16x8 kf[KS];
   {
     const bf16_t* krow = p.K + (size_t)(first + kl) * p.ldk + hc + 8 * half;
 #pragma unroll
     for (int s = 0; s < KS; ++s) kf[s] = kok ? *(const bf16x8*)(krow + 16 * s) : zero8();
-    TileLoadT<TILE, D> t;
-    t.load(p.V, p.ldv, first, k0, len, hc, tid);
-    t.store(sVf, KP, tid);
-    t.load(p.V, p.ldv, first, k0 + TILE, len, hc, tid);
-    t.store(sVf + TILE * KP, KP, tid);
+    if constexpr (WIN) {                       // a walk through a window is short: every load of the prologue is on its way before the first wait
+      RowsInTurn<BLK, D> t;
+      load_rows(t, p.V, p.ldv, first, k0, len, hc, tid);
+      load_rows(tq, p.Q, p.ldq, first, k0, len, wi_head * group * D, tid);
+      load_rows(td, p.dO, p.ldo, first, k0, len, wi_head * group * D, tid);
+      load_stats(wi_head * group, k0);
+      t.store(sVf, KP, tid);
+    } else {
+      TileLoadT<TILE, D> t;
+      t.load(p.V, p.ldv, first, k0, len, hc, tid);
+      t.store(sVf, KP, tid);
+      t.load(p.V, p.ldv, first, k0 + TILE, len, hc, tid);
+      t.store(sVf + TILE * KP, KP, tid);
+    }
   }
   const bf16_t* vfrag = sVf + (32 * wave + li) * KP + 8 * half;
   const float c = p.scale * LOG2E;
@@ -725,20 +743,13 @@ __global__ __launch_bounds__(256, 2) void k_attn_bwd_kv(AttnParams p) {
 #pragma unroll
     for (int j = 0; j < 16; ++j) { dk[dt][j] = 0.f; dv[dt][j] = 0.f; }
   const int wk_first = k0 + 32 * wave;
-  TileLoad<WIN, QT, D> tq, td;
-  float r_lse = 0.f, r_delta = 0.f;
   for (int g = 0; g < group; ++g) {             // every query head that reads this key/value head
   const int hq = wi_head * group + g, hcq = hq * D;
-  auto load_stats = [&](int qb) {
-    if (tid < QT) {
-      const bool ok = qb + tid < len;
-      r_lse = ok ? p.lse[(size_t)hq * p.T + first + qb + tid] * LOG2E : INFINITY;   // exp2(x - inf) = 0
-      r_delta = ok ? p.delta[(size_t)hq * p.T + first + qb + tid] : 0.f;
-    }
-  };
-  load_rows(tq, p.Q, p.ldq, first, k0, len, hcq, tid);
-  load_rows(td, p.dO, p.ldo, first, k0, len, hcq, tid);
-  load_stats(k0);
+  if (!WIN || g > 0) {
+    load_rows(tq, p.Q, p.ldq, first, k0, len, hcq, tid);
+    load_rows(td, p.dO, p.ldo, first, k0, len, hcq, tid);
+    load_stats(hq, k0);
+  }
   const int qend = WIN ? min(len, k0 + BLK - 1 + p.window) : len;
   for (int qb = k0; qb < qend; qb += QT) {      // queries before the block see none of its keys
     __syncthreads();
@@ -749,7 +760,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_bwd_kv(AttnParams p) {
     if (qb + QT < qend) {
       load_rows(tq, p.Q, p.ldq, first, qb + QT, len, hcq, tid);
       load_rows(td, p.dO, p.ldo, first, qb + QT, len, hcq, tid);
-      load_stats(qb + QT);
+      load_stats(hq, qb + QT);
     }
     if (qb + QT - 1 < wk_first) continue;     // every query of the tile lies before this wave's keys
     if (WIN && qb >= wk_first + 31 + p.window && wk_first >= p.n_sinks) continue;
