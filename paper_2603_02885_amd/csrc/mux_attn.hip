@@ -58,6 +58,7 @@ struct AttnParams {
   float scale;        // (comes with the arguments before it: behind the next two, a load of its own that the loops waited for, 41.9 us, 41.6)
   int n_blocks64, grid128;   // one-kernel backward: then as many of at most 64 tokens, from workgroup grid128 on
   int window, n_sinks;       // WIN kernels: query i sees key j <= i iff i - j < window or j < n_sinks
+  unsigned zero_from;        // WIN forward and dQ: workgroups from here on clear the padding rows of a 64-row work item each
   float* sinks;              // WIN backward: partial dK, dV of the first keys from far queries (see k_attn_sink_kv), null: none
 };
 // Whether a query sees the key `ahead` tokens before it
@@ -220,6 +221,15 @@ __device__ __forceinline__ void zero_pad_columns(bf16_t* tile, int rows, int pit
   }
 }
 
+// Zero on the padding rows of a 64-row work item, `width` columns of one output (256 threads)
+__device__ __forceinline__ void clear_padding(const AttnParams& p, int item, bf16_t* out, int64_t ld, int width) {
+  const ItemView it = load_item(p.dtab, 0, item);
+  const uint32_t* bits = (const uint32_t*)(p.dtab + p.dtab[DH_OFF_ITEM_BITS]) + 2 * item;
+  const uint64_t valid = (uint64_t)bits[0] | (uint64_t)bits[1] << 32;
+  for (int r = (int)threadIdx.x >> 6; r < it.nrows; r += 4)
+    if (!(valid >> r & 1))
+      for (int c = (int)threadIdx.x & 63; c < width / 8; c += 64) *(uint4*)(out + (size_t)(it.row0 + r) * ld + 8 * c) = uint4{0u, 0u, 0u, 0u};
+}
 // First tile of the keys that the window of some query from q0 on begins in
 __device__ __forceinline__ int window_tile(const AttnParams& p, int q0) { return max(0, q0 - p.window + 1) & ~(TILE - 1); }
 
@@ -230,6 +240,10 @@ __global__ __launch_bounds__(256, 2) void k_attn_fwd(AttnParams p) {
   constexpr int KS = Dim<D>::KS, DT = Dim<D>::DT, DP = Dim<D>::DP, KP = Dim<D>::KP, TP = Dim<D>::TP;
   __shared__ __align__(16) bf16_t sK[TILE * KP];
   __shared__ __align__(16) bf16_t sV[TILE * TP];
+  if (WIN && blockIdx.x >= p.zero_from) {
+    clear_padding(p, (int)(blockIdx.x - p.zero_from), p.Out, p.ldo, p.H * D);
+    return;
+  }
   int wi_block, wi_head;
   if (p.short_map) { if (!short_item<D>(blockIdx.x, p.n_blocks, p.H, wi_block, wi_head)) return; }
   else work_item(p.n_blocks, p.H, wi_block, wi_head);
@@ -451,6 +465,13 @@ __global__ __launch_bounds__(256, 2) void k_attn_bwd_q(AttnParams p) {
   constexpr int KS = Dim<D>::KS, DT = Dim<D>::DT, DP = Dim<D>::DP, KP = Dim<D>::KP, TP = Dim<D>::TP;
   __shared__ __align__(16) bf16_t sK[TILE * TP];
   __shared__ __align__(16) bf16_t sV[TILE * KP];
+  if (WIN && blockIdx.x >= p.zero_from) {
+    const int item = (int)(blockIdx.x - p.zero_from);
+    clear_padding(p, item, p.dQ, p.ldq, p.H * D);
+    clear_padding(p, item, p.dK, p.ldk, p.Hkv * D);
+    clear_padding(p, item, p.dV, p.ldv, p.Hkv * D);
+    return;
+  }
   int wi_block, wi_head;
   work_item(p.n_blocks, p.H, wi_block, wi_head);
   const int32_t* blk = p.dtab + p.list_off + (p.block0 + wi_block) * DA_WORDS;
@@ -860,9 +881,25 @@ struct ShortLds {
   __align__(16) bf16_t Q[QT * TP];
   __align__(16) bf16_t dO[QT * TP];
   __align__(16) bf16_t S[R * SP];
-  float lse[R], delta[R];
+  __align__(16) float delta[R];
+  float lse[R];
 };
-// WIN: the mask alone differs (a wave whose keys no query of a step sees forms zeros there).
+// WIN: the mask (a wave whose keys no query of a step sees forms zeros there), and what is subtracted from dP: sum_j P dP, from all the
+// keys, which are here, instead of dO . O from the stored O.  The rounding of O would be most of the error of dQ and dK in
+// sequences so short (64 tokens of 80 columns: 2.6e-3 of their norm, 2.4e-3 so, of which 1.7e-3 is the results' own rounding), and O is
+// not read; for that a barrier a step.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float dpp_add(float v) {
+  return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, ROWS, 0xf, false));
+}
+// Sum over the 32 lanes of a half-wave, in its lanes 16 .. 31
+__device__ __forceinline__ float sum_keys(float v) {
+  v = dpp_add<0xB1, 0xf>(v);       // lanes 1 apart
+  v = dpp_add<0x4E, 0xf>(v);       // 2 apart
+  v = dpp_add<0x141, 0xf>(v);      // mirrored in halves of a row
+  v = dpp_add<0x140, 0xf>(v);      // mirrored in a row
+  return dpp_add<0x142, 0xa>(v);   // the row before, into rows 1 and 3
+}
 template <int D, int R, bool WIN>
 __device__ __forceinline__ void attn_bwd_short(const AttnParams& p, const int wi_block, const int wi_head, const bool stored,
                                                const int tid, ShortLds<D, R>& lds) {
@@ -895,8 +932,11 @@ __device__ __forceinline__ void attn_bwd_short(const AttnParams& p, const int wi
     return kok ? p.lse[(size_t)hq * p.T + first + kl] * LOG2E : INFINITY;            // exp2(x - inf) = 0
   };
   auto store_stats = [&](float s, float lse2) {
-    s += __shfl_xor(s, 32);
-    if (half == 0) { sDelta[kl] = s; sLse[kl] = lse2; }
+    if (!WIN) s += __shfl_xor(s, 32);
+    if (half == 0) {
+      if (!WIN) sDelta[kl] = s;
+      sLse[kl] = lse2;
+    }
   };
   TileLoadT<QT, D, NTHR> tq, td;
   bf16x8 vf[KS];
@@ -904,8 +944,10 @@ __device__ __forceinline__ void attn_bwd_short(const AttnParams& p, const int wi
     TileLoadT<R, D, NTHR> t;
     t.load(p.K, p.ldk, first, 0, len, hc, tid);
     uint4 xd[KS], xo[KS];                      // every load of the prologue is on its way before the first wait
+    if (!WIN) {
 #pragma unroll
-    for (int st = 0; st < KS; ++st) { xd[st] = piece(p.dO, wi_head * group, st); xo[st] = piece(p.O, wi_head * group, st); }
+      for (int st = 0; st < KS; ++st) { xd[st] = piece(p.dO, wi_head * group, st); xo[st] = piece(p.O, wi_head * group, st); }
+    }
     const float lse2 = load_lse(wi_head * group);
     tq.load(p.Q, p.ldq, first, 0, len, wi_head * group * D, tid);
     td.load(p.dO, p.ldo, first, 0, len, wi_head * group * D, tid);
@@ -917,8 +959,10 @@ __device__ __forceinline__ void attn_bwd_short(const AttnParams& p, const int wi
     zero_pad_columns<D, DP, NTHR>(sD, QT, TP, tid);
     t.store(sK, TP, tid);
     float sum = 0.f;
+    if (!WIN) {
 #pragma unroll
-    for (int st = 0; st < KS; ++st) sum = dot(sum, xd[st], xo[st]);
+      for (int st = 0; st < KS; ++st) sum = dot(sum, xd[st], xo[st]);
+    }
     store_stats(sum, lse2);
   }
   const bf16_t* kfrag = sK + kl * TP + 8 * half;
@@ -932,8 +976,10 @@ __device__ __forceinline__ void attn_bwd_short(const AttnParams& p, const int wi
     const int hq = wi_head * group + g, hcq = hq * D;
     if (g > 0) {                               // (every read of the last head's statistics lies before its last barrier)
       float sum = 0.f;
+      if (!WIN) {
 #pragma unroll 2
-      for (int st = 0; st < KS; ++st) sum = dot(sum, piece(p.dO, hq, st), piece(p.O, hq, st));
+        for (int st = 0; st < KS; ++st) sum = dot(sum, piece(p.dO, hq, st), piece(p.O, hq, st));
+      }
       store_stats(sum, load_lse(hq));
     }
     for (int qb = 0; qb < len; qb += QT) {
@@ -950,8 +996,9 @@ __device__ __forceinline__ void attn_bwd_short(const AttnParams& p, const int wi
         }
       };
       if (!LATE) load_next();
-      if (qb + QT - 1 >= 32 * wave) {          // some query of the tile sees a key of this wave
-        f32x16 s, dp;
+      f32x16 s, dp;
+      const bool seen = qb + QT - 1 >= 32 * wave;      // some query of the tile sees a key of this wave
+      if (seen) {
 #pragma unroll
         for (int j = 0; j < 16; ++j) { s[j] = 0.f; dp[j] = 0.f; }
 #pragma unroll
@@ -976,8 +1023,34 @@ __device__ __forceinline__ void attn_bwd_short(const AttnParams& p, const int wi
           for (int j = 0; j < 16; ++j)
             if (8 * (j >> 2) + (j & 3) < rel) s[j] = 0.f;
         }
+        if constexpr (WIN) {
+          // This wave's part of sum_j P dP of every query: over the 32 lanes (keys) of a half, inside rows of 16 lanes, then the
+          // first row's sum into the second.
+          float part[16];
 #pragma unroll
-        for (int j = 0; j < 16; ++j) dp[j] = s[j] * (dp[j] - sDelta[qb + tok(j, half)]);   // dS
+          for (int j = 0; j < 16; ++j) part[j] = sum_keys(s[j] * dp[j]);
+          if (li == 16)
+#pragma unroll
+            for (int g4 = 0; g4 < 4; ++g4)
+              *(float4*)(sDelta + QT * wave + 8 * g4 + 4 * half) = float4{part[4 * g4], part[4 * g4 + 1], part[4 * g4 + 2], part[4 * g4 + 3]};
+        }
+      }
+      if (WIN) __syncthreads();
+      if (seen) {
+        if constexpr (WIN) {
+          float delta[16] = {};
+          for (int w = 0; w <= qb / QT && w < NW; ++w)         // the waves whose keys the tile sees, in order
+#pragma unroll
+            for (int g4 = 0; g4 < 4; ++g4) {
+              const float4 d = *(const float4*)(sDelta + QT * w + 8 * g4 + 4 * half);
+              delta[4 * g4] += d.x; delta[4 * g4 + 1] += d.y; delta[4 * g4 + 2] += d.z; delta[4 * g4 + 3] += d.w;
+            }
+#pragma unroll
+          for (int j = 0; j < 16; ++j) dp[j] = s[j] * (dp[j] - delta[j]);                  // dS
+        } else {
+#pragma unroll
+          for (int j = 0; j < 16; ++j) dp[j] = s[j] * (dp[j] - sDelta[qb + tok(j, half)]);   // dS
+        }
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
           const bf16x8 pb = pack8(s, u), ds = pack8(dp, u);
@@ -1222,7 +1295,8 @@ mux_status forward(const char* fn, const mux_attn_desc* desc, Window w, const mu
   p.list_off = st->dev_image[DH_ATT_OFF_FWD];
   ZeroParams z{};
   z.dtab = p.dtab; z.out[0] = (bf16_t*)O; z.ld[0] = desc->ldo; z.n_out = 1; z.width[0] = desc->n_heads * D;
-  if (st->valid_total < st->T)                // a table without padding rows has nothing to clear
+  const bool win = w.window > 0, pads = st->valid_total < st->T;
+  if (pads && !win)                           // a table without padding rows has nothing to clear
     MUX_LAUNCH("attn_zero_pad", k_attn_zero_pad, dim3((unsigned)st->items[0].size(), (unsigned)((z.width[0] + 2047) / 2048)), dim3(256), 0, stream, z);
   // Only short sequences and a multiple of eight heads: dealt as in the backward where neighbouring heads share cache lines,
   // heads share keys and values, or the pairs are many, eight a compute unit (40 heads of 80, 16 x 64 tokens 10.2 -> 9.5 us;
@@ -1232,8 +1306,10 @@ mux_status forward(const char* fn, const mux_attn_desc* desc, Window w, const mu
   p.short_map = st->n_attn_blocks64 + st->n_attn_blocks128 == st->n_attn_blocks && p.H % 8 == 0 &&
                 (D % 64 != 0 || p.H > p.Hkv || (int64_t)st->n_attn_blocks * p.H >= 8 * kComputeUnits);
   p.window = w.window; p.n_sinks = w.n_sinks;
+  p.zero_from = (unsigned)st->n_attn_blocks * (unsigned)desc->n_heads;
+  // (a workgroup more for the padding of each work item rather than a launch: 2112 tokens, 32/8 heads of 128, 34.7 -> 28.0 us)
   if (st->n_attn_blocks > 0)
-    ATTN_LAUNCH_WIN("attn_fwd", k_attn_fwd, D, w.window > 0, dim3((unsigned)st->n_attn_blocks * (unsigned)desc->n_heads), stream, p);
+    ATTN_LAUNCH_WIN("attn_fwd", k_attn_fwd, D, win, dim3(p.zero_from + (pads && win ? (unsigned)st->items[0].size() : 0u)), stream, p);
   return last_hip(fn);
 }
 
@@ -1269,12 +1345,12 @@ mux_status backward(const char* fn, const mux_attn_desc* desc, Window w, const m
   z.dtab = p.dtab; z.n_out = 3;
   z.width[0] = desc->n_heads * D; z.width[1] = z.width[2] = desc->n_kv_heads * D;
   z.out[0] = p.dQ; z.ld[0] = desc->ldq; z.out[1] = p.dK; z.ld[1] = desc->ldk; z.out[2] = p.dV; z.ld[2] = desc->ldv;
-  if (st->valid_total < st->T)
-    MUX_LAUNCH("attn_zero_pad", k_attn_zero_pad, dim3((unsigned)st->items[0].size(), (unsigned)((z.width[0] + 2047) / 2048)), dim3(256), 0, stream, z);
   int n64 = 0, n128 = 0, n_long = 0;
   plan_backward(st, desc, n_long, n128, n64);
+  const bool win = w.window > 0, pads = st->valid_total < st->T, ride = win && n_long > 0;
+  if (pads && !ride)
+    MUX_LAUNCH("attn_zero_pad", k_attn_zero_pad, dim3((unsigned)st->items[0].size(), (unsigned)((z.width[0] + 2047) / 2048)), dim3(256), 0, stream, z);
   p.list_off = st->dev_image[DH_ATT_OFF_BWD];
-  const bool win = w.window > 0;
   p.window = w.window; p.n_sinks = w.n_sinks;
   if (n_long > 0) {
     const size_t n = (size_t)st->T * desc->n_heads;
@@ -1292,7 +1368,8 @@ mux_status backward(const char* fn, const mux_attn_desc* desc, Window w, const m
     ATTN_LAUNCH_WIN("attn_bwd_kv", k_attn_bwd_kv, D, win, dim3((unsigned)n_long * (unsigned)desc->n_kv_heads), stream, p);
     AttnParams q = p;
     q.list_off = st->dev_image[DH_ATT_OFF_FWD];
-    ATTN_LAUNCH_WIN("attn_bwd_q", k_attn_bwd_q, D, win, dim3((unsigned)n_long * (unsigned)desc->n_heads), stream, q);
+    q.zero_from = (unsigned)n_long * (unsigned)desc->n_heads;
+    ATTN_LAUNCH_WIN("attn_bwd_q", k_attn_bwd_q, D, win, dim3(q.zero_from + (pads && ride ? (unsigned)st->items[0].size() : 0u)), stream, q);
   }
   if (n128 + n64 > 0) {
     p.block0 = n_long;
