@@ -64,6 +64,16 @@ def parse():
                          "sequences of the chosen workload (heads of --head-dim, as many as the q projection is wide)")
     ap.add_argument("--head-dim", type=int, default=128,
                     help="with --attention: head dimension (64, 80, 96 or 128); heads = projection width / head dimension")
+    ap.add_argument("--window", type=int, default=0,
+                    help="with --attention: sliding window of so many tokens (0: none); --sinks first tokens stay visible")
+    ap.add_argument("--sinks", type=int, default=4, help="with --attention --window: first tokens that stay visible")
+    ap.add_argument("--norm", action="store_true",
+                    help="instead of the benchmark line: layer norm of the chosen workload's rows, each task with its own "
+                         "weights, forward + backward at the width of the first projection's input, in GB/s")
+    ap.add_argument("--preference", action="store_true",
+                    help="instead of the benchmark line: the preference loss of the chosen workload's sequences, paired "
+                         "two by two inside a task (workloads 2, 4, 7, 8, 9), over --vocab logits a row, in GB/s")
+    ap.add_argument("--vocab", type=int, default=32000, help="with --preference: entries of the vocabulary")
     ap.add_argument("--dispatch", action="store_true",
                     help="instead of the benchmark line: Dispatch of the chosen workload's tokens (packed per task <-> "
                          "aligned batch) at the width of the first projection's input, in GB/s")
@@ -545,13 +555,18 @@ def attention(mx, torch, args):
     O, dO = torch.empty((T, H * d), device=dev, dtype=torch.bfloat16), rnd()
     desc = mx.AttnDesc(H, d, 3 * H * d, 3 * H * d, 3 * H * d, H * d)
     saved = torch.zeros(max(mx.mux_attn_saved_bytes(desc, st), 256), dtype=torch.uint8, device=dev)
-    wsb = mx.mux_attn_workspace_bytes(desc, st)
+    w, z = args.window, args.sinks
+    wsb = mx.mux_attn_window_workspace_bytes(desc, w, z, st) if w else mx.mux_attn_workspace_bytes(desc, st)
     ws = torch.zeros(max(wsb, 256), dtype=torch.uint8, device=dev)
     stream = torch.cuda.current_stream()
 
     def one():
-        mx.mux_attn_forward(desc, st, dtab, Q, K, V, O, saved, stream)
-        mx.mux_attn_backward(desc, st, dtab, Q, K, V, O, dO, saved, dQ, dK, dV, ws, wsb, stream)
+        if w:
+            mx.mux_attn_window_forward(desc, w, z, st, dtab, Q, K, V, O, saved, stream)
+            mx.mux_attn_window_backward(desc, w, z, st, dtab, Q, K, V, O, dO, saved, dQ, dK, dV, ws, wsb, stream)
+        else:
+            mx.mux_attn_forward(desc, st, dtab, Q, K, V, O, saved, stream)
+            mx.mux_attn_backward(desc, st, dtab, Q, K, V, O, dO, saved, dQ, dK, dV, ws, wsb, stream)
     for _ in range(args.warmup):
         one()
     torch.cuda.synchronize()
@@ -565,7 +580,8 @@ def attention(mx, torch, args):
     prof = mx.mux_profile_collect()
     mx.mux_profile_enable(0)
     lens = [n for t in wl.tasks for n in t.seq_lens]
-    pairs = float(sum(n * (n + 1) // 2 for n in lens)) * H
+    seen = lambda n: sum(min(i + 1, w) + min(z, max(0, i + 1 - w)) for i in range(n)) if w else n * (n + 1) // 2      # noqa: E731
+    pairs = float(sum(seen(n) for n in lens)) * H
     flops = {"attn_fwd": 4.0 * d * pairs, "attn_bwd_kv": 6.0 * d * pairs, "attn_bwd_q": 4.0 * d * pairs}
     kernels = {}
     for e in prof:
@@ -576,10 +592,11 @@ def attention(mx, torch, args):
         kernels[e["name"]] = k
     valid = mx.mux_segtab_valid_tokens(st)
     dom = max((n for n in kernels if n in flops), key=lambda n: kernels[n]["avg_us"])
-    return {"metric": "chunk-aligned causal attention fwd+bwd tokens/s", "value": valid / (ms * 1e-3), "unit": "tokens/s",
+    return {"metric": f"chunk-aligned {'windowed' if w else 'causal'} attention fwd+bwd tokens/s", "value": valid / (ms * 1e-3), "unit": "tokens/s",
             "n_gpus": 1, "steps": args.steps, "warmup": args.warmup, "ms_per_step": ms, "higher_is_better": True,
             "dtype": "bf16", "data": "synthetic",
-            "config": {"workload": f"configs[{args.workload}] {wl.name}: sequences of {wl.notes}; {H} heads of {d}",
+            "config": {"workload": f"configs[{args.workload}] {wl.name}: sequences of {wl.notes}; {H} heads of {d}" +
+                       (f", window {w}, {z} first tokens" if w else ""),
                        "rows": T, "valid_tokens": valid, "sequences": len(lens), "longest": max(lens)},
             "tflops": 14.0 * d * pairs / (ms * 1e-3) / 1e12,
             "roofline": {"kernel": dom, "bound": "mfma", "achieved": kernels[dom]["tflops"], "peak": PEAK_BF16_MFMA,
@@ -629,6 +646,97 @@ def dispatch(mx, torch, args):
             "dtype": "bf16", "data": "synthetic", "round_trip_bit_exact": bool(ok),
             "config": {"workload": f"configs[{args.workload}] {wl.name}", "rows": T, "valid_tokens": valid, "width": width},
             "kernels": res}
+
+
+def kernel_rates(mx, torch, args, one, nbytes):
+    """Warm-up, then args.steps calls of `one` with every kernel timed; `nbytes`: algorithmic bytes of a kernel by its name."""
+    for _ in range(args.warmup):
+        one()
+    torch.cuda.synchronize()
+    mx.mux_profile_enable(1)
+    mx.mux_profile_collect()
+    for _ in range(args.steps):
+        one()
+    torch.cuda.synchronize()
+    prof = mx.mux_profile_collect()
+    mx.mux_profile_enable(0)
+    res = {}
+    for e in prof:
+        k = res[e["name"]] = {"launches": e["launches"], "avg_us": e["total_ms"] * 1e3 / max(e["launches"], 1)}
+        if e["name"] in nbytes:
+            k["gbps"] = nbytes[e["name"]] / (e["total_ms"] * 1e-3 / args.steps) / 1e9
+            k["frac_of_hbm_peak"] = k["gbps"] / PEAK_HBM
+    return res
+
+
+def table_of(mx, torch, wl):
+    st = mx.mux_segtab_build([mx.TaskDesc(t.kind, t.rank, t.scale, t.seq_lens) for t in wl.tasks], wl.chunk, wl.max_pack_len, 0)
+    nb = mx.mux_segtab_device_bytes(st)
+    dtab = torch.zeros(nb, dtype=torch.uint8, device="cuda:0")
+    mx.mux_segtab_upload(st, dtab, nb)
+    torch.cuda.synchronize()
+    return st, dtab
+
+
+def norm(mx, torch, args):
+    """Layer norm of the workload's rows, bf16, every task with its own weights.  Algorithmic bytes: forward, every valid row
+    read and every row written once; backward, x and dy of every valid row read and dx of every row written once."""
+    import mux_workloads as wlm
+    wl = wlm.config(args.workload, seed=args.seed)
+    st, dtab = table_of(mx, torch, wl)
+    T, V, N, dev = mx.mux_segtab_rows(st), mx.mux_segtab_valid_tokens(st), wl.layers[0][1], "cuda:0"
+    rnd = lambda *s: torch.randn(s, device=dev).to(torch.bfloat16)                                  # noqa: E731
+    x, dy, y = rnd(T, N), rnd(T, N), rnd(T, N)
+    dx = torch.empty_like(x)
+    desc = mx.NormDesc(N, mx.MUX_DT_BF16, [rnd(N) for _ in wl.tasks], [rnd(N) for _ in wl.tasks])
+    grads = [[torch.empty(N, device=dev) for _ in wl.tasks] for _ in range(2)]
+    saved = torch.zeros(max(mx.mux_norm_saved_bytes(desc, st), 256), dtype=torch.uint8, device=dev)
+    wsb = mx.mux_norm_workspace_bytes(desc, st)
+    ws = torch.zeros(max(wsb, 256), dtype=torch.uint8, device=dev)
+    stream = torch.cuda.current_stream()
+
+    def one():
+        mx.mux_norm_forward(desc, st, dtab, x, y, saved, stream)
+        mx.mux_norm_backward(desc, st, dtab, x, dy, saved, dx, grads[0], grads[1], 0, ws, wsb, stream)
+    return {"metric": "layer norm of the aligned batch", "unit": "GB/s", "steps": args.steps, "warmup": args.warmup,
+            "dtype": "bf16", "data": "synthetic",
+            "config": {"workload": f"configs[{args.workload}] {wl.name}", "rows": T, "valid_tokens": V, "width": N},
+            "kernels": kernel_rates(mx, torch, args, one, {"norm_fwd": 2.0 * N * (V + T), "norm_bwd": 2.0 * N * (2 * V + T)})}
+
+
+def preference(mx, torch, args):
+    """Preference loss of the workload's sequences, paired two by two inside a task, every token counted, bf16 logits.
+    Algorithmic bytes: forward, the logits of every valid row read once; backward, read once and dlogits of every row written once."""
+    import mux_workloads as wlm
+    wl = wlm.config(args.workload, seed=args.seed)
+    pairs, at = [], 0
+    for t in wl.tasks:
+        pairs += [(at + i, at + i + 1, 0.1, 0.0) for i in range(0, len(t.seq_lens) - 1, 2)]
+        at += len(t.seq_lens)
+    if not pairs:
+        raise SystemExit(f"--preference: no task of workload {args.workload} has two sequences")
+    st, _ = table_of(mx, torch, wl)
+    T, tok, V, dev = mx.mux_segtab_rows(st), mx.mux_segtab_valid_tokens(st), args.vocab, "cuda:0"
+    logits = torch.empty((T, V), dtype=torch.bfloat16, device=dev).normal_(0.0, 2.5)
+    dlogits = torch.empty_like(logits)
+    labels = torch.randint(V, (T,), dtype=torch.int32, device=dev)
+    desc = mx.PrefDesc(V)
+    lay = torch.from_numpy(mx.mux_pref_layout(st, pairs)).to(dev)
+    logp, loss, dloss = torch.empty(at, device=dev), torch.empty(len(pairs), device=dev), torch.full((len(pairs),), 1.0 / len(pairs), device=dev)
+    saved = torch.zeros(mx.mux_pref_saved_bytes(desc, st, len(pairs)), dtype=torch.uint8, device=dev)
+    wsb = mx.mux_pref_workspace_bytes(desc, st)
+    ws = torch.zeros(wsb, dtype=torch.uint8, device=dev)
+    stream = torch.cuda.current_stream()
+    ref = torch.zeros(at, device=dev)
+
+    def one():
+        mx.mux_pref_forward(desc, st, lay, len(pairs), logits, labels, ref, None, logp, loss, saved, ws, wsb, stream)
+        mx.mux_pref_backward(desc, st, lay, len(pairs), logits, labels, saved, dloss, dlogits, stream)
+    return {"metric": "preference loss forward + backward", "unit": "GB/s", "steps": args.steps, "warmup": args.warmup,
+            "dtype": "bf16", "data": "synthetic",
+            "config": {"workload": f"configs[{args.workload}] {wl.name}", "rows": T, "valid_tokens": tok, "vocab": V,
+                       "sequences": at, "pairs": len(pairs)},
+            "kernels": kernel_rates(mx, torch, args, one, {"pref_rows": 2.0 * tok * V, "pref_bwd": 2.0 * V * (tok + T)})}
 
 
 def cpu_baseline(wl, seconds, seed, full_runs=True):
@@ -702,6 +810,12 @@ def main():
         return
     if args.attention:
         print(json.dumps(attention(mx, torch, args)))
+        return
+    if args.norm:
+        print(json.dumps(norm(mx, torch, args)))
+        return
+    if args.preference:
+        print(json.dumps(preference(mx, torch, args)))
         return
     if args.dispatch:
         print(json.dumps(dispatch(mx, torch, args)))
