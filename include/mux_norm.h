@@ -13,8 +13,8 @@
  * ldx elements between rows, Y, dY [T, width] with ldy, all of the storage type `dtype`, as are gamma_t and beta_t [width].
  * Statistics, sums and the gradients dgamma_t, dbeta_t are fp32 in both types.  Rows of padding: their content is ignored, Y
  * and dX are written as zero there.  Any width from 1 to MUX_NORM_MAX_WIDTH, any leading dimension >= width, any
- * pointers aligned to their element: rows that are whole 16-byte pieces at 16-byte aligned places (pointers and leading
- * dimensions too) are moved in such pieces, others element by element.
+ * pointers aligned to their element, fewer than 2^24 rows.  What lies between a row's width and its leading dimension is left as
+ * it is.
  * Y may be X itself and dX may be X or dY itself (same pointer, same leading dimension); other overlaps of what is
  * written with what is read, and dgamma / dbeta buffers that overlap each other, are refused (MUX_ERR_INVALID_ARG).
  */
@@ -43,7 +43,7 @@ typedef struct {
 } mux_norm_desc;
 
 /* Bytes of `saved` (forward -> backward: mean and rstd of every row, fp32 [2][T]) and of the backward's workspace (partial
- * sums of the weights' gradients).  Host arithmetic; 0 for arguments that the calls refuse. */
+ * sums of the weights' gradients).  Host arithmetic; 0 for a null argument or a width out of range. */
 size_t mux_norm_saved_bytes(const mux_norm_desc* desc, const mux_segtab* st);
 size_t mux_norm_workspace_bytes(const mux_norm_desc* desc, const mux_segtab* st);
 

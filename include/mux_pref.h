@@ -19,7 +19,9 @@
  * aligned to their element; dlogits may be the logits' own memory (same pointer, same leading dimension).  labels: device
  * int32 [T].  ref_logp, logp: device fp32 [number of sequences]; row_logp: device fp32 [T]; loss, dloss: device fp32
  * [n_pairs].  The content of rows that are not counted is never read.  Row maxima and sums over the vocabulary are fp32, sums over
- * a sequence's rows, margins and losses 64-bit until they are stored.  Infinite and NaN logits give what the formulas give.
+ * a sequence's rows, margins and losses 64-bit until they are stored.  A logit of -infinity has probability zero (as a label it
+ * makes L_s -infinity); a counted row that holds +infinity, NaN or nothing but -infinity makes lp_i, its sequence's sum and
+ * its pairs' losses NaN.  At most 2^24 slabs of 8 KB of a row in dlogits, 32 KB in the logits of a forward pass.
  */
 #ifndef MUX_PREF_H_
 #define MUX_PREF_H_

@@ -397,7 +397,8 @@ mux_status check(const char* fn, const mux_norm_desc* d, const mux_segtab* st) {
   if (d->ldx < d->width || d->ldy < d->width) return fail(MUX_ERR_SHAPE, std::string(fn) + ": a leading dimension is smaller than the width");
   if (d->n_tasks != st->n_tasks) return fail(MUX_ERR_SHAPE, std::string(fn) + ": descriptor and table disagree on the number of tasks");
   const int64_t ld = std::max(d->ldx, d->ldy);
-  if (ld >= ((int64_t)1 << 40) || (int64_t)st->T * ld >= ((int64_t)1 << 40)) return fail(MUX_ERR_SHAPE, std::string(fn) + ": problem too large");
+  // (a launch is held to 2^32 threads, at most 256 a row)
+  if (ld >= ((int64_t)1 << 40) || (int64_t)st->T * ld >= ((int64_t)1 << 40) || st->T >= 1 << 24) return fail(MUX_ERR_SHAPE, std::string(fn) + ": problem too large");
   return MUX_OK;
 }
 
@@ -521,7 +522,7 @@ mux_status last_hip(const char* fn) {
 using namespace mux;
 
 extern "C" size_t mux_norm_saved_bytes(const mux_norm_desc* desc, const mux_segtab* st) {
-  if (!desc || !st) return 0;
+  if (!desc || !st || desc->width < 1 || desc->width > MUX_NORM_MAX_WIDTH) return 0;
   return align256((size_t)st->T * 2 * sizeof(float));
 }
 

@@ -4,7 +4,7 @@
 // computed from them is one exponential an element.  A workgroup takes a slab of a row's vocabulary, so that a few rows fill the chip as
 // well as many do, and holds it in registers: maximum, then the sum of exponentials against it, one read.  The slabs' (maximum, sum)
 // pairs are joined by the launch that sums the rows of each sequence, a fixed number of terms in a fixed order; a third launch
-// forms the pairs' losses and slopes.  Rows that are not counted are never read.
+// forms the pairs' losses and slopes (few rows: one launch does both).  Rows that are not counted are never read.
 // Rows may begin anywhere (a vocabulary of odd size): what lies before a row's first 16-byte boundary and behind its last
 // belongs to the first and the last slab, element by element; the rest moves in 16-byte pieces.
 #include <algorithm>
@@ -336,9 +336,10 @@ mux_status check(const char* fn, const mux_pref_desc* d, const mux_segtab* st, i
   const int64_t ld = grad ? std::max(d->ld, d->ldg) : d->ld;
   if (d->ld < d->vocab || (grad && d->ldg < d->vocab)) return fail(MUX_ERR_SHAPE, std::string(fn) + ": a leading dimension is smaller than the vocabulary");
   int slabs, slab;
-  cut(d, std::min(kRowPieces, kGradPieces), slabs, slab);
-  if (ld >= ((int64_t)1 << 40) || (int64_t)st->T * ld >= ((int64_t)1 << 42) || (int64_t)st->T * slabs >= ((int64_t)1 << 31) ||
-      n_pairs > (1 << 28))
+  cut(d, grad ? kGradPieces : kRowPieces, slabs, slab);
+  // (a launch is held to 2^32 threads: 137 GB of logits for the gradient, 550 GB forward)
+  if (ld >= ((int64_t)1 << 40) || (int64_t)st->T * ld >= ((int64_t)1 << 42) ||
+      (int64_t)st->T * slabs * kThreads >= ((int64_t)1 << 32) || n_pairs > (1 << 28))
     return fail(MUX_ERR_SHAPE, std::string(fn) + ": problem too large");
   return MUX_OK;
 }

@@ -226,6 +226,21 @@ def test_special_values(env):
     assert np.isfinite(d[:9]).all() and np.isnan(d[16:25]).all() and np.isfinite(d[32:36]).all()
 
 
+def test_rows_without_a_probability(env):
+    """A row that holds +inf, or nothing but -inf, makes its own sequence and its pairs NaN and nothing else."""
+    inf = float("inf")
+    for vocab, dtype in ((300, 0), (9001, 1)):
+        c = Case(env, [[4, 5], [6, 3], [2, 2]], 16, vocab, dtype, [(0, 1, 0.5, 0.0), (2, 3, 0.5, 0.0), (4, 5, 0.5, 0.0)], seed=13, answers=1.1)
+        c.x[1, vocab - 1] = inf
+        c.x[17] = -inf
+        c.forward()
+        c.backward()
+        loss, logp, d = c.host(c.loss), c.host(c.logp), c.host(c.dx)
+        assert np.isnan(loss[:2]).all() and np.isfinite(loss[2])
+        assert np.isnan(logp[[0, 2]]).all() and np.isfinite(logp[[1, 3, 4, 5]]).all()
+        assert np.isnan(d[:9]).all() and np.isnan(d[16:25]).all() and np.isfinite(d[32:36]).all()
+
+
 def test_repeats_streams_and_capture(env):
     c = Case(env, LENS, 16, 9001, 0, PAIRS, seed=11)
     c.forward()

@@ -147,6 +147,22 @@ def test_norm_refusals(mx):
     mx.mux_norm_forward(mx.NormDesc(8, 0, n_tasks=0), empty, None, None, None, None)
 
 
+def test_launches_that_would_not_fit(mx):
+    """A launch is held to 2^32 threads: what would take more is refused before anything runs."""
+    M = 1 << 40
+    st = mx.mux_segtab_build([mx.TaskDesc(0, 0, 1.0, [(1 << 24) - 256]), mx.TaskDesc(0, 0, 1.0, [1])], 256)
+    assert mx.mux_segtab_rows(st) == 1 << 24
+    d = mx.NormDesc(1, 0, n_tasks=2)
+    refused(mx, 2, lambda: mx.mux_norm_forward(d, st, M, 2 * M, 3 * M, None))
+    refused(mx, 2, lambda: mx.mux_norm_backward(d, st, M, 2 * M, 3 * M, 4 * M, 5 * M, None, None, 0, None, 0))
+    e = mx.PrefDesc(1)
+    refused(mx, 2, lambda: mx.mux_pref_forward(e, st, M, 0, 2 * M, 3 * M, None, None, None, None, None, 4 * M, 1 << 60))
+    refused(mx, 2, lambda: mx.mux_pref_backward(e, st, M, 0, 2 * M, 3 * M, 4 * M, None, 5 * M))
+    st = mx.mux_segtab_build([mx.TaskDesc(0, 0, 1.0, [64])], 64)
+    e = mx.PrefDesc(1 << 30)                                       # 2^18 slabs of the gradient a row, 2^16 of the forward
+    refused(mx, 2, lambda: mx.mux_pref_backward(e, st, M, 0, 2 * M, 3 * M, 4 * M, None, 5 * M))
+
+
 def test_pref_refusals(mx):
     st = mx.mux_segtab_build([mx.TaskDesc(0, 0, 1.0, [5, 6])], 16)
     M = 1 << 20
