@@ -60,6 +60,8 @@ struct AttnParams {
   int window, n_sinks;       // WIN kernels: query i sees key j <= i iff i - j < window or j < n_sinks
   unsigned zero_from;        // WIN forward and dQ: workgroups from here on clear the padding rows of a 64-row work item each
   float* sinks;              // WIN backward: partial dK, dV of the first keys from far queries (see k_attn_sink_kv), null: none
+  int kv_parts, n_long;      // WIN backward: workgroups that share a key block's walk, blocks of the launch
+  float* parts;              // .. and their partial dK, dV, [block][key/value head][part] (see part_at)
 };
 // Whether a query sees the key `ahead` tokens before it
 __device__ __forceinline__ bool in_window(const AttnParams& p, int ahead, bool sink) {
@@ -461,13 +463,18 @@ __global__ __launch_bounds__(256) void k_attn_delta(AttnParams p) {
 }
 
 // ------------------------------------------------------------------------------------------------ dQ
+template <int D> __device__ void join_parts(const AttnParams& p, int id);      // (with dK, dV below)
+
 template <int D, bool WIN>
 __global__ __launch_bounds__(256, 2) void k_attn_bwd_q(AttnParams p) {
   constexpr int KS = Dim<D>::KS, DT = Dim<D>::DT, DP = Dim<D>::DP, KP = Dim<D>::KP, TP = Dim<D>::TP;
   __shared__ __align__(16) bf16_t sK[TILE * TP];
   __shared__ __align__(16) bf16_t sV[TILE * KP];
   if (WIN && blockIdx.x >= p.zero_from) {
-    const int item = (int)(blockIdx.x - p.zero_from);
+    int item = (int)(blockIdx.x - p.zero_from);
+    const int joins = p.kv_parts > 1 ? p.n_long * p.Hkv * DT : 0;
+    if (item < joins) { join_parts<D>(p, item); return; }
+    item -= joins;
     clear_padding(p, item, p.dQ, p.ldq, p.H * D);
     clear_padding(p, item, p.dK, p.ldk, p.Hkv * D);
     clear_padding(p, item, p.dV, p.ldv, p.Hkv * D);
@@ -710,7 +717,67 @@ __global__ __launch_bounds__(256, 2) void k_attn_sink_kv(AttnParams p) {
 }
 
 // ------------------------------------------------------------------------------------------------ dK, dV
+// Partial dK (which = 0) and dV (1) of a key block and head: accumulator elements 4 jg .. 4 jg + 3 of thread tid in one 16-byte piece
+template <int D>
+__device__ __forceinline__ float* part_at(const AttnParams& p, int block, int head, int part, int dt, int jg, int which, int tid) {
+  return p.parts + ((((size_t)block * p.Hkv + head) * p.kv_parts + part) * (Dim<D>::DT * 8) + (dt * 4 + jg) * 2 + which) * 1024 + 4 * tid;
+}
+// dK and dV of the lane's key, columns 32 dt .. of the head: what the sequence's far queries add to the first keys, then the rows
+template <int D>
+__device__ __forceinline__ void add_sinks(const AttnParams& p, const int32_t* blk, int head, int kl, int half, int dt, f32x16& dk, f32x16& dv) {
+  if (p.sinks == nullptr || kl >= p.n_sinks) return;         // (these keys lie in the first block of their sequence)
+  const int len = blk[DA_LEN], far = sink_far(p, len);
+  for (int b = far / SINK_SPAN * SINK_SPAN; b < len && far < len; b += SINK_SPAN) {
+    const float* part = p.sinks + sink_part<D>(p, blk[DA_SINK_SLOT] + b / SINK_SPAN, head) + (size_t)kl * D + 4 * half;
+#pragma unroll
+    for (int jg = 0; jg < 4; ++jg) {
+      if (32 * dt + 8 * jg >= D) continue;
+      const float4 a = *(const float4*)(part + 32 * dt + 8 * jg), v = *(const float4*)(part + (size_t)p.n_sinks * D + 32 * dt + 8 * jg);
+      dk[4 * jg + 0] += a.x; dk[4 * jg + 1] += a.y; dk[4 * jg + 2] += a.z; dk[4 * jg + 3] += a.w;
+      dv[4 * jg + 0] += v.x; dv[4 * jg + 1] += v.y; dv[4 * jg + 2] += v.z; dv[4 * jg + 3] += v.w;
+    }
+  }
+}
+template <int D>
+__device__ __forceinline__ void store_kv(const AttnParams& p, int row, int hc, int half, int dt, const f32x16& dk, const f32x16& dv) {
+  bf16_t* krow = p.dK + (size_t)row * p.ldk + hc;
+  bf16_t* vrow = p.dV + (size_t)row * p.ldv + hc;
+#pragma unroll
+  for (int jg = 0; jg < 4; ++jg) {
+    if (32 * dt + 8 * jg >= D) continue;      // the unused half of the last 32 columns
+    uint2 a, b;
+    a.x = pack_bf16x2(dk[4 * jg + 0] * p.scale, dk[4 * jg + 1] * p.scale);
+    a.y = pack_bf16x2(dk[4 * jg + 2] * p.scale, dk[4 * jg + 3] * p.scale);
+    b.x = pack_bf16x2(dv[4 * jg + 0], dv[4 * jg + 1]);
+    b.y = pack_bf16x2(dv[4 * jg + 2], dv[4 * jg + 3]);
+    *(uint2*)(krow + 32 * dt + 8 * jg + 4 * half) = a;
+    *(uint2*)(vrow + 32 * dt + 8 * jg + 4 * half) = b;
+  }
+}
+// The parts of a key block's walk added in their order, 32 columns of a head (256 threads)
+template <int D>
+__device__ void join_parts(const AttnParams& p, int id) {
+  const int dt = id % Dim<D>::DT, head = id / Dim<D>::DT % p.Hkv, block = id / Dim<D>::DT / p.Hkv;
+  const int32_t* blk = p.dtab + p.dtab[DH_ATT_OFF_BWD] + block * DA_WORDS;
+  const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, kl = blk[DA_BLOCK0] + 32 * (tid >> 6) + (lane & 31);
+  f32x16 dk, dv;
+#pragma unroll
+  for (int j = 0; j < 16; ++j) dk[j] = dv[j] = 0.f;
+  for (int i = 0; i < p.kv_parts; ++i)
+#pragma unroll
+    for (int jg = 0; jg < 4; ++jg) {
+      if (32 * dt + 8 * jg >= D) continue;
+      const float4 a = *(const float4*)part_at<D>(p, block, head, i, dt, jg, 0, tid), v = *(const float4*)part_at<D>(p, block, head, i, dt, jg, 1, tid);
+      dk[4 * jg + 0] += a.x; dk[4 * jg + 1] += a.y; dk[4 * jg + 2] += a.z; dk[4 * jg + 3] += a.w;
+      dv[4 * jg + 0] += v.x; dv[4 * jg + 1] += v.y; dv[4 * jg + 2] += v.z; dv[4 * jg + 3] += v.w;
+    }
+  add_sinks<D>(p, blk, head, kl, half, dt, dk, dv);
+  if (kl < blk[DA_LEN]) store_kv<D>(p, blk[DA_FIRST_ROW] + kl, head * D, half, dt, dk, dv);
+}
+
 // WIN: a key block walks the queries up to its last key's window; what the first keys get from those beyond comes from k_attn_sink_kv.
+// Where the blocks are few, a walk (over the queries of every head of the group) is cut into kv_parts runs of steps, a workgroup
+// each, whose fp32 sums join_parts adds beside dQ.
 template <int D, bool WIN>
 __global__ __launch_bounds__(256, 2) void k_attn_bwd_kv(AttnParams p) {
   constexpr int KS = Dim<D>::KS, DT = Dim<D>::DT, DP = Dim<D>::DP, KP = Dim<D>::KP, TP = Dim<D>::TP;
@@ -719,12 +786,25 @@ __global__ __launch_bounds__(256, 2) void k_attn_bwd_kv(AttnParams p) {
   __shared__ __align__(16) bf16_t sD[QT * TP];
   __shared__ __align__(16) bf16_t sVf[BLK * KP];   // the block's own V rows (B operand of dO V^T), kept here to save registers
   __shared__ float sLse[QT], sDelta[QT];
-  int wi_block, wi_head;                       // wi_head: a key/value head
-  work_item(p.n_blocks, p.Hkv, wi_block, wi_head);
+  int wi_block, wi_head, part = 0;             // wi_head: a key/value head
+  work_item(p.n_blocks, WIN ? p.Hkv * p.kv_parts : p.Hkv, wi_block, wi_head);
+  if constexpr (WIN) { part = wi_head % p.kv_parts; wi_head /= p.kv_parts; }
   const int32_t* blk = p.dtab + p.list_off + (p.block0 + wi_block) * DA_WORDS;
   const int first = blk[DA_FIRST_ROW], len = blk[DA_LEN], k0 = blk[DA_BLOCK0];
   const int hc = wi_head * D;
   const int group = p.H / p.Hkv;
+  const int qend = WIN ? min(len, k0 + BLK - 1 + p.window) : len;
+  // the part's run: from query qfirst of head g0 of the group to before query qlast of head g1
+  int g0 = 0, g1 = group - 1, qfirst = k0, qlast = qend;
+  if (WIN && p.kv_parts > 1) {
+    const int steps = (qend - k0 + QT - 1) / QT;
+    const int u0 = (int)((int64_t)group * steps * part / p.kv_parts), u1 = (int)((int64_t)group * steps * (part + 1) / p.kv_parts);
+    g0 = min(u0 / steps, group - 1);
+    g1 = (u1 + steps - 1) / steps - 1;
+    qfirst = k0 + QT * (u0 - g0 * steps);
+    qlast = min(qend, k0 + QT * (u1 - g1 * steps));
+    if (u0 == u1) { g1 = g0 - 1; qfirst = k0; }              // (a short walk: nothing left for this part)
+  }
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, li = lane & 31, half = lane >> 5;
   const int kl = k0 + 32 * wave + li;          // this lane's key inside the sequence
   const bool kok = kl < len;
@@ -747,9 +827,9 @@ __global__ __launch_bounds__(256, 2) void k_attn_bwd_kv(AttnParams p) {
     if constexpr (WIN) {                       // a walk through a window is short: every load of the prologue is on its way before the first wait
       RowsInTurn<BLK, D> t;
       load_rows(t, p.V, p.ldv, first, k0, len, hc, tid);
-      load_rows(tq, p.Q, p.ldq, first, k0, len, wi_head * group * D, tid);
-      load_rows(td, p.dO, p.ldo, first, k0, len, wi_head * group * D, tid);
-      load_stats(wi_head * group, k0);
+      load_rows(tq, p.Q, p.ldq, first, qfirst, len, (wi_head * group + g0) * D, tid);
+      load_rows(td, p.dO, p.ldo, first, qfirst, len, (wi_head * group + g0) * D, tid);
+      load_stats(wi_head * group + g0, qfirst);
       t.store(sVf, KP, tid);
     } else {
       TileLoadT<TILE, D> t;
@@ -767,21 +847,21 @@ __global__ __launch_bounds__(256, 2) void k_attn_bwd_kv(AttnParams p) {
 #pragma unroll
     for (int j = 0; j < 16; ++j) { dk[dt][j] = 0.f; dv[dt][j] = 0.f; }
   const int wk_first = k0 + 32 * wave;
-  for (int g = 0; g < group; ++g) {             // every query head that reads this key/value head
+  for (int g = g0; g <= g1; ++g) {              // every query head that reads this key/value head
   const int hq = wi_head * group + g, hcq = hq * D;
-  if (!WIN || g > 0) {
+  if (!WIN || g > g0) {
     load_rows(tq, p.Q, p.ldq, first, k0, len, hcq, tid);
     load_rows(td, p.dO, p.ldo, first, k0, len, hcq, tid);
     load_stats(hq, k0);
   }
-  const int qend = WIN ? min(len, k0 + BLK - 1 + p.window) : len;
-  for (int qb = k0; qb < qend; qb += QT) {      // queries before the block see none of its keys
+  const int stop = g == g1 ? qlast : qend;
+  for (int qb = g == g0 ? qfirst : k0; qb < stop; qb += QT) {      // queries before the block see none of its keys
     __syncthreads();
     tq.store(sQ, TP, tid);
     td.store(sD, TP, tid);
     if (tid < QT) { sLse[tid] = r_lse; sDelta[tid] = r_delta; }
     __syncthreads();
-    if (qb + QT < qend) {
+    if (qb + QT < stop) {
       load_rows(tq, p.Q, p.ldq, first, qb + QT, len, hcq, tid);
       load_rows(td, p.dO, p.ldo, first, qb + QT, len, hcq, tid);
       load_stats(hq, qb + QT);
@@ -830,37 +910,21 @@ __global__ __launch_bounds__(256, 2) void k_attn_bwd_kv(AttnParams p) {
     }
   }
   }                                             // next query head of the group
-  if (WIN && p.sinks != nullptr && kl < p.n_sinks) {         // (these keys lie in the first block of their sequence)
-    const int far = sink_far(p, len);
-    for (int b = far / SINK_SPAN * SINK_SPAN; b < len && far < len; b += SINK_SPAN) {
-      const float* part = p.sinks + sink_part<D>(p, blk[DA_SINK_SLOT] + b / SINK_SPAN, wi_head) + (size_t)kl * D + 4 * half;
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-        for (int jg = 0; jg < 4; ++jg) {
-          if (32 * dt + 8 * jg >= D) continue;
-          const float4 a = *(const float4*)(part + 32 * dt + 8 * jg), v = *(const float4*)(part + (size_t)p.n_sinks * D + 32 * dt + 8 * jg);
-          dk[dt][4 * jg + 0] += a.x; dk[dt][4 * jg + 1] += a.y; dk[dt][4 * jg + 2] += a.z; dk[dt][4 * jg + 3] += a.w;
-          dv[dt][4 * jg + 0] += v.x; dv[dt][4 * jg + 1] += v.y; dv[dt][4 * jg + 2] += v.z; dv[dt][4 * jg + 3] += v.w;
-        }
-    }
-  }
-  if (kok) {
-    bf16_t* krow = p.dK + (size_t)(first + kl) * p.ldk + hc;
-    bf16_t* vrow = p.dV + (size_t)(first + kl) * p.ldv + hc;
+  if (WIN && p.kv_parts > 1) {
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
       for (int jg = 0; jg < 4; ++jg) {
-        if (32 * dt + 8 * jg >= D) continue;      // the unused half of the last 32 columns
-        uint2 a, b;
-        a.x = pack_bf16x2(dk[dt][4 * jg + 0] * p.scale, dk[dt][4 * jg + 1] * p.scale);
-        a.y = pack_bf16x2(dk[dt][4 * jg + 2] * p.scale, dk[dt][4 * jg + 3] * p.scale);
-        b.x = pack_bf16x2(dv[dt][4 * jg + 0], dv[dt][4 * jg + 1]);
-        b.y = pack_bf16x2(dv[dt][4 * jg + 2], dv[dt][4 * jg + 3]);
-        *(uint2*)(krow + 32 * dt + 8 * jg + 4 * half) = a;
-        *(uint2*)(vrow + 32 * dt + 8 * jg + 4 * half) = b;
+        if (32 * dt + 8 * jg >= D) continue;
+        *(float4*)part_at<D>(p, wi_block, wi_head, part, dt, jg, 0, tid) = float4{dk[dt][4 * jg + 0], dk[dt][4 * jg + 1], dk[dt][4 * jg + 2], dk[dt][4 * jg + 3]};
+        *(float4*)part_at<D>(p, wi_block, wi_head, part, dt, jg, 1, tid) = float4{dv[dt][4 * jg + 0], dv[dt][4 * jg + 1], dv[dt][4 * jg + 2], dv[dt][4 * jg + 3]};
       }
+    return;
+  }
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) {
+    if (WIN) add_sinks<D>(p, blk, wi_head, kl, half, dt, dk[dt], dv[dt]);
+    if (kok) store_kv<D>(p, first + kl, hc, half, dt, dk[dt], dv[dt]);
   }
 }
 
@@ -1316,6 +1380,33 @@ mux_status forward(const char* fn, const mux_attn_desc* desc, Window w, const mu
   return last_hip(fn);
 }
 
+// Workgroups that share a key block's walk.  Places are two a compute unit; with fewer workgroups than places the launch takes the
+// longest walk, with more their total and about half a walk until the last is done.  Beside that, in steps of 32 queries (1.4 to 2.3
+// us): the parts' sums, 128 KB each at 128 columns, 1 to 5 while all have a place and are read back from the caches, some 20 more for every chip
+// full after that; and a part walks three steps at least.  Window 1024, heads of 128, backward, walk in one part -> in n: 2048 tokens, 8 heads a
+// key/value head and 4 of those (64 workgroups), 8 parts 700 -> 259 us; 4096 tokens, 4 and 8 (256), 2 parts 471 -> 373, 3 parts 416; window 300, 3000 tokens, 4
+// and 6 (144), 3 parts 177 -> 126, 4 parts 139; window 2048, 16384 + 9001 tokens, 4 and 4 (796), 2 parts 1985 -> 1787, 3 parts 1879; window 512, 9600
+// tokens, 4 and 8 (600), 2 parts 617 -> 616, 3 parts 625.
+int kv_parts(const mux_segtab* st, const mux_attn_desc* desc, Window w, int n_long) {
+  if (w.window == 0 || n_long == 0) return 1;
+  const double wgs = (double)n_long * desc->n_kv_heads, group = desc->n_heads / desc->n_kv_heads;
+  const double walk = group * (double)((std::min<int64_t>(st->attn_longest, (int64_t)w.window + kAttnBlockRows - 1) + 31) / 32);
+  int best = 1;
+  double least = 0;
+  for (int n = 1; n <= 16 && (n == 1 || 3 * n <= walk); ++n) {
+    const double full = wgs * n / (2 * kComputeUnits);
+    const double cost = (full <= 1 ? walk / n : full * walk / n + walk / (2 * n)) + (n == 1 ? 0 : full <= 1 ? 1 + 4 * full : 5 + 20 * (full - 1));
+    if (n == 1 || cost < least) { best = n; least = cost; }
+  }
+  return best;
+}
+// Bytes of their partial sums
+size_t part_bytes(const mux_attn_desc* desc, const mux_segtab* st, Window w) {
+  int n_long, n128, n64;
+  plan_backward(st, desc, n_long, n128, n64);
+  const int parts = kv_parts(st, desc, w, n_long);
+  return parts > 1 ? (size_t)n_long * (size_t)desc->n_kv_heads * (size_t)parts * ((size_t)(desc->head_dim + 31) / 32 * 8) * 4096 : 0;
+}
 // Bytes of the partial dK, dV of the first keys (see k_attn_sink_kv), behind the fp32 [n_heads][T] of the workspace.
 size_t sink_bytes(const mux_attn_desc* desc, const mux_segtab* st, Window w) {
   if (w.n_sinks == 0 || st->attn_longest <= kAttnBlockRows - 1 + w.window) return 0;
@@ -1333,9 +1424,9 @@ mux_status backward(const char* fn, const mux_attn_desc* desc, Window w, const m
   const void* ptrs[8] = {Q, K, V, O, dO, dQ, dK, dV};
   for (const void* q : ptrs)
     if (!aligned16(q)) return fail(MUX_ERR_UNSUPPORTED, std::string(fn) + ": pointers must be 16-byte aligned");
-  const size_t nsink = sink_bytes(desc, st, w);
-  if (ws_bytes < mux_attn_workspace_bytes(desc, st) + nsink) return fail(MUX_ERR_WORKSPACE, std::string(fn) + ": workspace too small");
-  if (nsink > 0 && !aligned16(ws)) return fail(MUX_ERR_UNSUPPORTED, std::string(fn) + ": the workspace must be 16-byte aligned");
+  const size_t nsink = sink_bytes(desc, st, w), npart = part_bytes(desc, st, w);
+  if (ws_bytes < mux_attn_workspace_bytes(desc, st) + nsink + npart) return fail(MUX_ERR_WORKSPACE, std::string(fn) + ": workspace too small");
+  if (nsink + npart > 0 && !aligned16(ws)) return fail(MUX_ERR_UNSUPPORTED, std::string(fn) + ": the workspace must be 16-byte aligned");
   hipStream_t stream = (hipStream_t)hip_stream;
   const int D = desc->head_dim;
   AttnParams p{};
@@ -1369,11 +1460,15 @@ mux_status backward(const char* fn, const mux_attn_desc* desc, Window w, const m
       q.sinks = p.sinks;
       ATTN_LAUNCH("attn_sink_kv", k_attn_sink_kv, D, dim3((unsigned)q.n_blocks * (unsigned)(desc->n_kv_heads * ((w.n_sinks + 31) / 32))), stream, q);
     }
-    ATTN_LAUNCH_WIN("attn_bwd_kv", k_attn_bwd_kv, D, win, dim3((unsigned)n_long * (unsigned)desc->n_kv_heads), stream, p);
+    p.n_long = n_long;
+    p.kv_parts = kv_parts(st, desc, w, n_long);
+    p.parts = (float*)((char*)ws + mux_attn_workspace_bytes(desc, st) + nsink);
+    const unsigned kv_items = (unsigned)n_long * (unsigned)desc->n_kv_heads;
+    ATTN_LAUNCH_WIN("attn_bwd_kv", k_attn_bwd_kv, D, win, dim3(kv_items * (unsigned)p.kv_parts), stream, p);
     AttnParams q = p;
     q.list_off = st->dev_image[DH_ATT_OFF_FWD];
     q.zero_from = (unsigned)n_long * (unsigned)desc->n_heads;
-    ATTN_LAUNCH_WIN("attn_bwd_q", k_attn_bwd_q, D, win, dim3(q.zero_from + (pads && ride ? (unsigned)st->items[0].size() : 0u)), stream, q);
+    ATTN_LAUNCH_WIN("attn_bwd_q", k_attn_bwd_q, D, win, dim3(q.zero_from + (p.kv_parts > 1 ? kv_items * (unsigned)((D + 31) / 32) : 0u) + (pads && ride ? (unsigned)st->items[0].size() : 0u)), stream, q);
   }
   if (n128 + n64 > 0) {
     p.block0 = n_long;
@@ -1420,7 +1515,8 @@ extern "C" mux_status mux_attn_backward(const mux_attn_desc* desc, const mux_seg
 extern "C" size_t mux_attn_window_workspace_bytes(const mux_attn_desc* desc, int32_t window, int32_t n_sinks, const mux_segtab* st) {
   if (!desc || !st || desc->n_heads < 1 || desc->n_kv_heads < 1 || desc->head_dim < 1 || window < 1 || n_sinks < 0 || n_sinks > MUX_ATTN_MAX_SINKS)
     return 0;
-  return mux_attn_workspace_bytes(desc, st) + sink_bytes(desc, st, effective(st, window, n_sinks));
+  const Window w = effective(st, window, n_sinks);
+  return mux_attn_workspace_bytes(desc, st) + sink_bytes(desc, st, w) + part_bytes(desc, st, w);
 }
 
 extern "C" mux_status mux_attn_window_forward(const mux_attn_desc* desc, int32_t window, int32_t n_sinks, const mux_segtab* st,
