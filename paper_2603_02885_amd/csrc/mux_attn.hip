@@ -59,9 +59,11 @@ struct AttnParams {
   int n_blocks64, grid128;   // one-kernel backward: then as many of at most 64 tokens, from workgroup grid128 on
   int window, n_sinks;       // WIN kernels: query i sees key j <= i iff i - j < window or j < n_sinks
   unsigned zero_from;        // WIN forward and dQ: workgroups from here on clear the padding rows of a 64-row work item each
-  float* sinks;              // WIN backward: partial dK, dV of the first keys from far queries (see k_attn_sink_kv), null: none
   int kv_parts, n_long;      // WIN backward: workgroups that share a key block's walk, blocks of the launch
   float* parts;              // .. and their partial dK, dV, [block][key/value head][part] (see part_at)
+  float *far, *near;         // WIN backward: partial dK, dV of the first keys from far and from near queries (see walk_sinks), null: none
+  unsigned sink_wgs;         // .. workgroups of the dK, dV launch that walk the far ones, a multiple of 8
+  int n_spans, sink_parts;   // .. spans of far queries, workgroups that share one
 };
 // Whether a query sees the key `ahead` tokens before it
 __device__ __forceinline__ bool in_window(const AttnParams& p, int ahead, bool sink) {
@@ -106,8 +108,7 @@ __device__ __forceinline__ int tok(int j, int half) { return 8 * (j >> 2) + 4 * 
 // Work item of a workgroup: (block of the list, head).  Workgroups go to the eight XCDs round-robin; with a multiple of
 // eight heads every XCD takes its own heads and walks the list in order, so that the blocks running on an XCD at one
 // time belong to two or three sequences of one head and find their keys and values in that XCD's L2.
-__device__ __forceinline__ void work_item(int n_blocks, int n_heads, int& block, int& head) {
-  const unsigned id = blockIdx.x;
+__device__ __forceinline__ void work_item(int n_blocks, int n_heads, int& block, int& head, unsigned id = blockIdx.x) {
   if ((n_heads & 7) == 0) {
     const unsigned j = id >> 3;
     head = (int)(id & 7) + 8 * (int)(j / (unsigned)n_blocks);
@@ -464,6 +465,7 @@ __global__ __launch_bounds__(256) void k_attn_delta(AttnParams p) {
 
 // ------------------------------------------------------------------------------------------------ dQ
 template <int D> __device__ void join_parts(const AttnParams& p, int id);      // (with dK, dV below)
+template <int D> __device__ void join_sinks(const AttnParams& p, int id);
 
 template <int D, bool WIN>
 __global__ __launch_bounds__(256, 2) void k_attn_bwd_q(AttnParams p) {
@@ -475,6 +477,9 @@ __global__ __launch_bounds__(256, 2) void k_attn_bwd_q(AttnParams p) {
     const int joins = p.kv_parts > 1 ? p.n_long * p.Hkv * DT : 0;
     if (item < joins) { join_parts<D>(p, item); return; }
     item -= joins;
+    const int sinks = p.far ? p.n_spans * p.Hkv : 0;
+    if (item < sinks) { join_sinks<D>(p, item); return; }
+    item -= sinks;
     clear_padding(p, item, p.dQ, p.ldq, p.H * D);
     clear_padding(p, item, p.dK, p.ldk, p.Hkv * D);
     clear_padding(p, item, p.dV, p.ldv, p.Hkv * D);
@@ -586,31 +591,51 @@ __global__ __launch_bounds__(256, 2) void k_attn_bwd_q(AttnParams p) {
 // ------------------------------------------------------------------------------------------------ dK, dV of the first keys
 // Every query of a sequence sees its first n_sinks keys.  What they get from the queries of the first key block's own walk
 // (k_attn_bwd_kv) is formed there; for the rest that walk would be as long as the sequence, one workgroup's while all others walk a
-// window.  So the queries from sink_far on are cut into spans of SINK_SPAN: one workgroup a span, 32 keys and a key/value
-// head, its waves take 32 queries at a time each (no barrier in the loop, tiles of their own in LDS), their sums are
-// added in LDS in a fixed order and the span's fp32 rows go to the workspace, where the first block's workgroup adds them in order.
-// 17637 tokens, 40 heads of 128, 4 first keys: 74 us, nearly all of it the queries and dO read once more (361 MB, 4.9 TB/s).  Spans of 2, 4, 8
-// blocks: 90, 75, 64 us, but one sequence of 16384 tokens with 32 / 8 heads 57, 72, 122.
+// window.  So the queries from sink_far on are cut into spans of SINK_SPAN: sink_parts workgroups a span, 32 keys and a key/value
+// head, at the head of the same launch, its waves take 32 queries at a time each (no barrier in the loop, tiles of their own in LDS),
+// their sums are added in LDS in a fixed order and the fp32 rows go to the workspace, as do the first block's own of these keys;
+// join_sinks adds them in order, beside dQ.  (In a launch of their own, the first block's workgroup adding what they left: window 1024, 4 first
+// keys, 17637 tokens, 40 heads of 128, backward 1512 us, 1515 now; 16384 + 9001 tokens, 16 / 4 heads, window 2048, 1826, 1592; 2048 tokens, 32 / 4
+// heads 246, 170; 500 tokens, 4 / 1 heads, window 64, 68, 32.)
 constexpr int SINK_SPAN = kAttnSinkSpan * BLK, SINK_TILE = 32;
 __device__ __forceinline__ int sink_far(const AttnParams& p, int len) {       // first query behind the first block's walk
   return min(len, (BLK - 1 + p.window + SINK_TILE - 1) / SINK_TILE * SINK_TILE);
 }
+// The rows [key][dK: D, dV: D] apart, of one of `n` that share a slot: [slot][i][key/value head][dK, dV][n_sinks][D]
 template <int D>
-__device__ __forceinline__ size_t sink_part(const AttnParams& p, int slot, int head) {
-  return ((size_t)slot * p.Hkv + head) * (size_t)p.n_sinks * (2 * D);
+__device__ __forceinline__ size_t sink_part(const AttnParams& p, int slot, int n, int i, int head) {
+  return (((size_t)slot * n + i) * p.Hkv + head) * (size_t)p.n_sinks * (2 * D);
+}
+// A lane's columns 32 dt .. of dK and dV, `out` its row and its first column
+template <int D>
+__device__ __forceinline__ void put_sums(float* out, int n_sinks, int dt, const f32x16& dk, const f32x16& dv) {
+#pragma unroll
+  for (int jg = 0; jg < 4; ++jg) {
+    if (32 * dt + 8 * jg >= D) continue;
+    *(float4*)(out + 32 * dt + 8 * jg) = float4{dk[4 * jg + 0], dk[4 * jg + 1], dk[4 * jg + 2], dk[4 * jg + 3]};
+    *(float4*)(out + (size_t)n_sinks * D + 32 * dt + 8 * jg) = float4{dv[4 * jg + 0], dv[4 * jg + 1], dv[4 * jg + 2], dv[4 * jg + 3]};
+  }
 }
 template <int D>
-__global__ __launch_bounds__(256, 2) void k_attn_sink_kv(AttnParams p) {
+struct SinkLds {
+  bf16_t tiles[4][2][SINK_TILE * Dim<D>::TP];
+  float2 stats[4][SINK_TILE];
+};
+template <int D>
+__device__ __forceinline__ void walk_sinks(const AttnParams& p, SinkLds<D>& lds) {
   constexpr int KS = Dim<D>::KS, DT = Dim<D>::DT, DP = Dim<D>::DP, TP = Dim<D>::TP, QT = SINK_TILE;
-  __shared__ __align__(16) bf16_t tiles[4][2][QT * TP];
-  __shared__ float2 stats[4][QT];
-  static_assert(sizeof(tiles) >= 2 * sizeof(float) * 32 * D, "the sums fit the tiles");
-  const int n_kt = (p.n_sinks + 31) / 32;
+  static_assert(sizeof(lds.tiles) >= 2 * sizeof(float) * 32 * D, "the sums fit the tiles");
+  auto& tiles = lds.tiles;
+  auto& stats = lds.stats;
+  const int n_kt = (p.n_sinks + 31) / 32, n_heads = p.Hkv * n_kt * p.sink_parts;
+  if (blockIdx.x >= (unsigned)p.n_spans * (unsigned)n_heads) return;
   int wi_block, wi_head;
-  work_item(p.n_blocks, p.Hkv * n_kt, wi_block, wi_head);
+  work_item(p.n_spans, n_heads, wi_block, wi_head);
+  const int part = wi_head % p.sink_parts;
+  wi_head /= p.sink_parts;
   const int kt = wi_head % n_kt;
   wi_head /= n_kt;
-  const int32_t* blk = p.dtab + p.list_off + wi_block * DA_WORDS;
+  const int32_t* blk = p.dtab + p.dtab[DH_ATT_OFF_SPANS] + wi_block * DA_WORDS;
   const int first = blk[DA_FIRST_ROW], len = blk[DA_LEN], span0 = blk[DA_BLOCK0];
   const int far = sink_far(p, len), qbegin = max(span0, far), qend = min(len, span0 + SINK_SPAN);
   if (qbegin >= qend) return;
@@ -652,7 +677,8 @@ __global__ __launch_bounds__(256, 2) void k_attn_sink_kv(AttnParams p) {
       st = float2{p.lse[at] * LOG2E, p.delta[at]};
     }
   };
-  for (int i = 0; i < group * tiles_a_head; ++i) {
+  const int turns = group * tiles_a_head;
+  for (int i = turns * part / p.sink_parts; i < turns * (part + 1) / p.sink_parts; ++i) {
     load(i);
     wave_sync();
     tq.store(sQ, TP, lane);
@@ -703,16 +729,38 @@ __global__ __launch_bounds__(256, 2) void k_attn_sink_kv(AttnParams p) {
     __syncthreads();
   }
   if (wave == 0 && kl < p.n_sinks) {
-    float* part = p.sinks + sink_part<D>(p, blk[DA_SINK_SLOT], wi_head) + (size_t)kl * D + 4 * half;
+    float* out = p.far + sink_part<D>(p, blk[DA_SINK_SLOT], p.sink_parts, part, wi_head) + (size_t)kl * D + 4 * half;
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-      for (int jg = 0; jg < 4; ++jg) {
-        if (32 * dt + 8 * jg >= D) continue;
-        *(float4*)(part + 32 * dt + 8 * jg) = float4{dk[dt][4 * jg + 0], dk[dt][4 * jg + 1], dk[dt][4 * jg + 2], dk[dt][4 * jg + 3]};
-        *(float4*)(part + (size_t)p.n_sinks * D + 32 * dt + 8 * jg) =
-            float4{dv[dt][4 * jg + 0], dv[dt][4 * jg + 1], dv[dt][4 * jg + 2], dv[dt][4 * jg + 3]};
-      }
+    for (int dt = 0; dt < DT; ++dt) put_sums<D>(out, p.n_sinks, dt, dk[dt], dv[dt]);
+  }
+}
+// Every part's rows of a sequence's first keys added in their order: near ones, far ones (256 threads)
+template <int D>
+__device__ void join_sinks(const AttnParams& p, int id) {
+  const int head = id % p.Hkv;
+  const int32_t* blk = p.dtab + p.dtab[DH_ATT_OFF_SPANS] + id / p.Hkv * DA_WORDS;
+  const int first = blk[DA_FIRST_ROW], len = blk[DA_LEN], far = sink_far(p, len);
+  if (blk[DA_BLOCK0] != 0 || far >= len) return;             // (a sequence once; without far queries the first block has stored its rows)
+  const int slot = blk[DA_SINK_SLOT], rows = p.n_sinks * (D / 4);
+  const int n0 = far / SINK_SPAN * p.sink_parts, n1 = (len + SINK_SPAN - 1) / SINK_SPAN * p.sink_parts;
+  const size_t step = (size_t)p.Hkv * p.n_sinks * (2 * D);
+  for (int e = threadIdx.x; e < 2 * rows; e += 256) {
+    float4 s{0.f, 0.f, 0.f, 0.f};
+    auto add = [&](const float* q) {
+      const float4 a = *(const float4*)q;
+      s.x += a.x; s.y += a.y; s.z += a.z; s.w += a.w;
+    };
+    const float* q = p.near + sink_part<D>(p, slot, p.kv_parts, 0, head) + 4 * e;
+#pragma unroll 4
+    for (int i = 0; i < p.kv_parts; ++i) add(q + i * step);
+    q = p.far + sink_part<D>(p, slot, p.sink_parts, 0, head) + 4 * e;
+#pragma unroll 4
+    for (int i = n0; i < n1; ++i) add(q + i * step);
+    const bool v = e >= rows;
+    const int at = v ? e - rows : e, key = at / (D / 4), col = head * D + at % (D / 4) * 4;
+    const float f = v ? 1.f : p.scale;
+    *(uint2*)((v ? p.dV + (size_t)(first + key) * p.ldv : p.dK + (size_t)(first + key) * p.ldk) + col) =
+        uint2{pack_bf16x2(s.x * f, s.y * f), pack_bf16x2(s.z * f, s.w * f)};
   }
 }
 
@@ -722,22 +770,11 @@ template <int D>
 __device__ __forceinline__ float* part_at(const AttnParams& p, int block, int head, int part, int dt, int jg, int which, int tid) {
   return p.parts + ((((size_t)block * p.Hkv + head) * p.kv_parts + part) * (Dim<D>::DT * 8) + (dt * 4 + jg) * 2 + which) * 1024 + 4 * tid;
 }
-// dK and dV of the lane's key, columns 32 dt .. of the head: what the sequence's far queries add to the first keys, then the rows
-template <int D>
-__device__ __forceinline__ void add_sinks(const AttnParams& p, const int32_t* blk, int head, int kl, int half, int dt, f32x16& dk, f32x16& dv) {
-  if (p.sinks == nullptr || kl >= p.n_sinks) return;         // (these keys lie in the first block of their sequence)
-  const int len = blk[DA_LEN], far = sink_far(p, len);
-  for (int b = far / SINK_SPAN * SINK_SPAN; b < len && far < len; b += SINK_SPAN) {
-    const float* part = p.sinks + sink_part<D>(p, blk[DA_SINK_SLOT] + b / SINK_SPAN, head) + (size_t)kl * D + 4 * half;
-#pragma unroll
-    for (int jg = 0; jg < 4; ++jg) {
-      if (32 * dt + 8 * jg >= D) continue;
-      const float4 a = *(const float4*)(part + 32 * dt + 8 * jg), v = *(const float4*)(part + (size_t)p.n_sinks * D + 32 * dt + 8 * jg);
-      dk[4 * jg + 0] += a.x; dk[4 * jg + 1] += a.y; dk[4 * jg + 2] += a.z; dk[4 * jg + 3] += a.w;
-      dv[4 * jg + 0] += v.x; dv[4 * jg + 1] += v.y; dv[4 * jg + 2] += v.z; dv[4 * jg + 3] += v.w;
-    }
-  }
+// Whether the key is one that join_sinks stores
+__device__ __forceinline__ bool joined_later(const AttnParams& p, int key, int len) {
+  return p.far != nullptr && key < p.n_sinks && sink_far(p, len) < len;
 }
+// dK and dV of a key, columns 32 dt .. of its head
 template <int D>
 __device__ __forceinline__ void store_kv(const AttnParams& p, int row, int hc, int half, int dt, const f32x16& dk, const f32x16& dv) {
   bf16_t* krow = p.dK + (size_t)row * p.ldk + hc;
@@ -771,24 +808,38 @@ __device__ void join_parts(const AttnParams& p, int id) {
       dk[4 * jg + 0] += a.x; dk[4 * jg + 1] += a.y; dk[4 * jg + 2] += a.z; dk[4 * jg + 3] += a.w;
       dv[4 * jg + 0] += v.x; dv[4 * jg + 1] += v.y; dv[4 * jg + 2] += v.z; dv[4 * jg + 3] += v.w;
     }
-  add_sinks<D>(p, blk, head, kl, half, dt, dk, dv);
-  if (kl < blk[DA_LEN]) store_kv<D>(p, blk[DA_FIRST_ROW] + kl, head * D, half, dt, dk, dv);
+  if (kl < blk[DA_LEN] && !joined_later(p, kl, blk[DA_LEN])) store_kv<D>(p, blk[DA_FIRST_ROW] + kl, head * D, half, dt, dk, dv);
 }
 
-// WIN: a key block walks the queries up to its last key's window; what the first keys get from those beyond comes from k_attn_sink_kv.
+// WIN: a key block walks the queries up to its last key's window; what the first keys get from those beyond comes from walk_sinks, for
+// which the launch's first workgroups are.
 // Where the blocks are few, a walk (over the queries of every head of the group) is cut into kv_parts runs of steps, a workgroup
 // each, whose fp32 sums join_parts adds beside dQ.
 template <int D, bool WIN>
 __global__ __launch_bounds__(256, 2) void k_attn_bwd_kv(AttnParams p) {
   constexpr int KS = Dim<D>::KS, DT = Dim<D>::DT, DP = Dim<D>::DP, KP = Dim<D>::KP, TP = Dim<D>::TP;
   constexpr int QT = 32;                       // queries staged per step
-  __shared__ __align__(16) bf16_t sQ[QT * TP];
-  __shared__ __align__(16) bf16_t sD[QT * TP];
-  __shared__ __align__(16) bf16_t sVf[BLK * KP];   // the block's own V rows (B operand of dO V^T), kept here to save registers
-  __shared__ float sLse[QT], sDelta[QT];
+  struct Lds {
+    bf16_t q[QT * TP], d[QT * TP];
+    bf16_t v[BLK * KP];                          // the block's own V rows (B operand of dO V^T), kept here to save registers
+    float lse[QT], delta[QT];
+  };
+  __shared__ __align__(16) char lds_bytes[WIN && sizeof(SinkLds<D>) > sizeof(Lds) ? sizeof(SinkLds<D>) : sizeof(Lds)];
+  Lds& lds = *(Lds*)lds_bytes;
+  bf16_t *const sQ = lds.q, *const sD = lds.d, *const sVf = lds.v;
+  float *const sLse = lds.lse, *const sDelta = lds.delta;
   int wi_block, wi_head, part = 0;             // wi_head: a key/value head
-  work_item(p.n_blocks, WIN ? p.Hkv * p.kv_parts : p.Hkv, wi_block, wi_head);
-  if constexpr (WIN) { part = wi_head % p.kv_parts; wi_head /= p.kv_parts; }
+  if constexpr (WIN) {
+    if (blockIdx.x < p.sink_wgs) {
+      walk_sinks<D>(p, *(SinkLds<D>*)lds_bytes);
+      return;
+    }
+    work_item(p.n_blocks, p.Hkv * p.kv_parts, wi_block, wi_head, blockIdx.x - p.sink_wgs);
+    part = wi_head % p.kv_parts;
+    wi_head /= p.kv_parts;
+  } else {
+    work_item(p.n_blocks, p.Hkv, wi_block, wi_head);
+  }
   const int32_t* blk = p.dtab + p.list_off + (p.block0 + wi_block) * DA_WORDS;
   const int first = blk[DA_FIRST_ROW], len = blk[DA_LEN], k0 = blk[DA_BLOCK0];
   const int hc = wi_head * D;
@@ -910,6 +961,12 @@ __global__ __launch_bounds__(256, 2) void k_attn_bwd_kv(AttnParams p) {
     }
   }
   }                                             // next query head of the group
+  const bool later = WIN && joined_later(p, kl, len);
+  if (later) {
+    float* out = p.near + sink_part<D>(p, blk[DA_SINK_SLOT], p.kv_parts, part, wi_head) + (size_t)kl * D + 4 * half;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) put_sums<D>(out, p.n_sinks, dt, dk[dt], dv[dt]);
+  }
   if (WIN && p.kv_parts > 1) {
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
@@ -921,11 +978,9 @@ __global__ __launch_bounds__(256, 2) void k_attn_bwd_kv(AttnParams p) {
       }
     return;
   }
+  if (kok && !later)
 #pragma unroll
-  for (int dt = 0; dt < DT; ++dt) {
-    if (WIN) add_sinks<D>(p, blk, wi_head, kl, half, dt, dk[dt], dv[dt]);
-    if (kok) store_kv<D>(p, first + kl, hc, half, dt, dk[dt], dv[dt]);
-  }
+    for (int dt = 0; dt < DT; ++dt) store_kv<D>(p, first + kl, hc, half, dt, dk[dt], dv[dt]);
 }
 
 // ------------------------------------------------------------------------------------------------ short sequences
@@ -1400,17 +1455,30 @@ int kv_parts(const mux_segtab* st, const mux_attn_desc* desc, Window w, int n_lo
   }
   return best;
 }
-// Bytes of their partial sums
-size_t part_bytes(const mux_attn_desc* desc, const mux_segtab* st, Window w) {
-  int n_long, n128, n64;
-  plan_backward(st, desc, n_long, n128, n64);
-  const int parts = kv_parts(st, desc, w, n_long);
-  return parts > 1 ? (size_t)n_long * (size_t)desc->n_kv_heads * (size_t)parts * ((size_t)(desc->head_dim + 31) / 32 * 8) * 4096 : 0;
-}
-// Bytes of the partial dK, dV of the first keys (see k_attn_sink_kv), behind the fp32 [n_heads][T] of the workspace.
-size_t sink_bytes(const mux_attn_desc* desc, const mux_segtab* st, Window w) {
-  if (w.n_sinks == 0 || st->attn_longest <= kAttnBlockRows - 1 + w.window) return 0;
-  return align256((size_t)st->n_attn_spans * (size_t)desc->n_kv_heads * (size_t)w.n_sinks * 2 * (size_t)desc->head_dim * sizeof(float));
+// How the dK, dV launch is cut, and where its partial sums lie behind the fp32 [n_heads][T] of the workspace.
+struct KvPlan {
+  int n_long, n128, n64, parts, sink_parts;
+  unsigned sink_wgs;               // 0: no far queries
+  size_t near, far, part, bytes;   // bytes: of the whole workspace
+};
+KvPlan plan_kv(const mux_attn_desc* desc, const mux_segtab* st, Window w) {
+  KvPlan k{};
+  plan_backward(st, desc, k.n_long, k.n128, k.n64);
+  k.parts = kv_parts(st, desc, w, k.n_long);
+  k.sink_parts = 1;
+  const size_t hkv = (size_t)desc->n_kv_heads, D = (size_t)desc->head_dim;
+  k.bytes = mux_attn_workspace_bytes(desc, st);
+  if (w.n_sinks > 0 && st->attn_longest > kAttnBlockRows - 1 + w.window) {
+    // a workgroup for every compute unit where spans are few, of one turn of 4 x 32 queries at least
+    const int64_t wgs = (int64_t)st->n_attn_spans * desc->n_kv_heads * ((w.n_sinks + 31) / 32), turns = (int64_t)(desc->n_heads / desc->n_kv_heads) * kAttnSinkSpan;
+    k.sink_parts = (int)std::max<int64_t>(1, std::min(kComputeUnits / wgs, turns));
+    k.sink_wgs = (unsigned)((wgs * k.sink_parts + 7) / 8 * 8);
+    const size_t one = (size_t)st->n_attn_spans * hkv * (size_t)w.n_sinks * 2 * D * sizeof(float);
+    k.near = k.bytes; k.bytes += align256(one * (size_t)k.parts);
+    k.far = k.bytes; k.bytes += align256(one * (size_t)k.sink_parts);
+  }
+  if (k.parts > 1) { k.part = k.bytes; k.bytes += (size_t)k.n_long * hkv * (size_t)k.parts * ((D + 31) / 32 * 8) * 4096; }
+  return k;
 }
 
 mux_status backward(const char* fn, const mux_attn_desc* desc, Window w, const mux_segtab* st, const void* dev_segtab, const void* Q,
@@ -1424,9 +1492,9 @@ mux_status backward(const char* fn, const mux_attn_desc* desc, Window w, const m
   const void* ptrs[8] = {Q, K, V, O, dO, dQ, dK, dV};
   for (const void* q : ptrs)
     if (!aligned16(q)) return fail(MUX_ERR_UNSUPPORTED, std::string(fn) + ": pointers must be 16-byte aligned");
-  const size_t nsink = sink_bytes(desc, st, w), npart = part_bytes(desc, st, w);
-  if (ws_bytes < mux_attn_workspace_bytes(desc, st) + nsink + npart) return fail(MUX_ERR_WORKSPACE, std::string(fn) + ": workspace too small");
-  if (nsink + npart > 0 && !aligned16(ws)) return fail(MUX_ERR_UNSUPPORTED, std::string(fn) + ": the workspace must be 16-byte aligned");
+  const KvPlan plan = plan_kv(desc, st, w);
+  if (ws_bytes < plan.bytes) return fail(MUX_ERR_WORKSPACE, std::string(fn) + ": workspace too small");
+  if (plan.near + plan.part > 0 && !aligned16(ws)) return fail(MUX_ERR_UNSUPPORTED, std::string(fn) + ": the workspace must be 16-byte aligned");
   hipStream_t stream = (hipStream_t)hip_stream;
   const int D = desc->head_dim;
   AttnParams p{};
@@ -1441,8 +1509,7 @@ mux_status backward(const char* fn, const mux_attn_desc* desc, Window w, const m
   z.dtab = p.dtab; z.n_out = 3;
   z.width[0] = desc->n_heads * D; z.width[1] = z.width[2] = desc->n_kv_heads * D;
   z.out[0] = p.dQ; z.ld[0] = desc->ldq; z.out[1] = p.dK; z.ld[1] = desc->ldk; z.out[2] = p.dV; z.ld[2] = desc->ldv;
-  int n64 = 0, n128 = 0, n_long = 0;
-  plan_backward(st, desc, n_long, n128, n64);
+  const int n64 = plan.n64, n128 = plan.n128, n_long = plan.n_long;
   const bool win = w.window > 0, pads = st->valid_total < st->T, ride = win && n_long > 0;
   if (pads && !ride)
     MUX_LAUNCH("attn_zero_pad", k_attn_zero_pad, dim3((unsigned)st->items[0].size(), (unsigned)((z.width[0] + 2047) / 2048)), dim3(256), 0, stream, z);
@@ -1452,23 +1519,22 @@ mux_status backward(const char* fn, const mux_attn_desc* desc, Window w, const m
     const size_t n = (size_t)st->T * desc->n_heads;
     p.n_blocks = n_long;
     ATTN_LAUNCH("attn_delta", k_attn_delta, D, dim3((unsigned)(((n + 3) / 4 * 16 + 255) / 256)), stream, p);
-    if (nsink > 0) {
-      AttnParams q = p;
-      q.n_blocks = st->n_attn_spans;
-      q.list_off = st->dev_image[DH_ATT_OFF_SPANS];
-      p.sinks = (float*)((char*)ws + mux_attn_workspace_bytes(desc, st));
-      q.sinks = p.sinks;
-      ATTN_LAUNCH("attn_sink_kv", k_attn_sink_kv, D, dim3((unsigned)q.n_blocks * (unsigned)(desc->n_kv_heads * ((w.n_sinks + 31) / 32))), stream, q);
-    }
     p.n_long = n_long;
-    p.kv_parts = kv_parts(st, desc, w, n_long);
-    p.parts = (float*)((char*)ws + mux_attn_workspace_bytes(desc, st) + nsink);
+    p.kv_parts = plan.parts; p.sink_parts = plan.sink_parts;
+    p.n_spans = st->n_attn_spans;
+    p.sink_wgs = plan.sink_wgs;
+    if (plan.parts > 1) p.parts = (float*)((char*)ws + plan.part);
+    if (plan.sink_wgs > 0) { p.near = (float*)((char*)ws + plan.near); p.far = (float*)((char*)ws + plan.far); }
     const unsigned kv_items = (unsigned)n_long * (unsigned)desc->n_kv_heads;
-    ATTN_LAUNCH_WIN("attn_bwd_kv", k_attn_bwd_kv, D, win, dim3(kv_items * (unsigned)p.kv_parts), stream, p);
+    ATTN_LAUNCH_WIN("attn_bwd_kv", k_attn_bwd_kv, D, win, dim3(p.sink_wgs + kv_items * (unsigned)p.kv_parts), stream, p);
     AttnParams q = p;
     q.list_off = st->dev_image[DH_ATT_OFF_FWD];
     q.zero_from = (unsigned)n_long * (unsigned)desc->n_heads;
-    ATTN_LAUNCH_WIN("attn_bwd_q", k_attn_bwd_q, D, win, dim3(q.zero_from + (p.kv_parts > 1 ? kv_items * (unsigned)((D + 31) / 32) : 0u) + (pads && ride ? (unsigned)st->items[0].size() : 0u)), stream, q);
+    unsigned wgs = q.zero_from;
+    if (p.kv_parts > 1) wgs += kv_items * (unsigned)((D + 31) / 32);
+    if (p.far) wgs += (unsigned)p.n_spans * (unsigned)desc->n_kv_heads;
+    if (pads && ride) wgs += (unsigned)st->items[0].size();
+    ATTN_LAUNCH_WIN("attn_bwd_q", k_attn_bwd_q, D, win, dim3(wgs), stream, q);
   }
   if (n128 + n64 > 0) {
     p.block0 = n_long;
@@ -1515,8 +1581,7 @@ extern "C" mux_status mux_attn_backward(const mux_attn_desc* desc, const mux_seg
 extern "C" size_t mux_attn_window_workspace_bytes(const mux_attn_desc* desc, int32_t window, int32_t n_sinks, const mux_segtab* st) {
   if (!desc || !st || desc->n_heads < 1 || desc->n_kv_heads < 1 || desc->head_dim < 1 || window < 1 || n_sinks < 0 || n_sinks > MUX_ATTN_MAX_SINKS)
     return 0;
-  const Window w = effective(st, window, n_sinks);
-  return mux_attn_workspace_bytes(desc, st) + sink_bytes(desc, st, w) + part_bytes(desc, st, w);
+  return plan_kv(desc, st, effective(st, window, n_sinks)).bytes;
 }
 
 extern "C" mux_status mux_attn_window_forward(const mux_attn_desc* desc, int32_t window, int32_t n_sinks, const mux_segtab* st,
