@@ -12,6 +12,7 @@
 // ds_read_b64_tr_b16.  A sum over 16 tokens may take them in any order as long as both operands agree; the order
 // used is the one the accumulator layout gives: slot i of half-wave h <-> token 8 (i / 4) + 4 h + i % 4.
 // Every output element has one owner; nothing is accumulated across workgroups, results repeat bit for bit.
+#include <algorithm>
 #include <type_traits>
 
 #include "mux_attn.h"
@@ -58,11 +59,12 @@ struct AttnParams {
   float scale;        // (comes with the arguments before it: behind the next two, a load of its own that the loops waited for, 41.9 us, 41.6)
   int n_blocks64, grid128;   // one-kernel backward: then as many of at most 64 tokens, from workgroup grid128 on
   int window, n_sinks;       // WIN kernels: query i sees key j <= i iff i - j < window or j < n_sinks
-  unsigned zero_from;        // WIN forward and dQ: workgroups from here on clear the padding rows of a 64-row work item each
-  int kv_parts, n_long;      // WIN backward: workgroups that share a key block's walk, blocks of the launch
+  unsigned zero_from;        // WIN: workgroups from here on clear the padding rows of a 64-row work item each
+  int kv_parts;              // WIN backward: workgroups that share a key block's walk
   float* parts;              // .. and their partial dK, dV, [block][key/value head][part] (see part_at)
   float *far, *near;         // WIN backward: partial dK, dV of the first keys from far and from near queries (see walk_sinks), null: none
-  unsigned sink_wgs;         // .. workgroups of the dK, dV launch that walk the far ones, a multiple of 8
+  unsigned sink_wgs, kv_wgs; // .. workgroups that walk the far ones and, behind them, those of dK and dV
+  unsigned q_from;           // .. first workgroup of dQ (sink_wgs, q_from: multiples of 8, so that an XCD keeps its heads)
   int n_spans, sink_parts;   // .. spans of far queries, workgroups that share one
 };
 // Whether a query sees the key `ahead` tokens before it
@@ -464,30 +466,17 @@ __global__ __launch_bounds__(256) void k_attn_delta(AttnParams p) {
 }
 
 // ------------------------------------------------------------------------------------------------ dQ
-template <int D> __device__ void join_parts(const AttnParams& p, int id);      // (with dK, dV below)
-template <int D> __device__ void join_sinks(const AttnParams& p, int id);
-
+template <int D>
+struct QLds {
+  bf16_t k[TILE * Dim<D>::TP], v[TILE * Dim<D>::KP];
+};
 template <int D, bool WIN>
-__global__ __launch_bounds__(256, 2) void k_attn_bwd_q(AttnParams p) {
+__device__ __forceinline__ void walk_keys(const AttnParams& p, QLds<D>& lds, unsigned id, int list_off) {
   constexpr int KS = Dim<D>::KS, DT = Dim<D>::DT, DP = Dim<D>::DP, KP = Dim<D>::KP, TP = Dim<D>::TP;
-  __shared__ __align__(16) bf16_t sK[TILE * TP];
-  __shared__ __align__(16) bf16_t sV[TILE * KP];
-  if (WIN && blockIdx.x >= p.zero_from) {
-    int item = (int)(blockIdx.x - p.zero_from);
-    const int joins = p.kv_parts > 1 ? p.n_long * p.Hkv * DT : 0;
-    if (item < joins) { join_parts<D>(p, item); return; }
-    item -= joins;
-    const int sinks = p.far ? p.n_spans * p.Hkv : 0;
-    if (item < sinks) { join_sinks<D>(p, item); return; }
-    item -= sinks;
-    clear_padding(p, item, p.dQ, p.ldq, p.H * D);
-    clear_padding(p, item, p.dK, p.ldk, p.Hkv * D);
-    clear_padding(p, item, p.dV, p.ldv, p.Hkv * D);
-    return;
-  }
+  bf16_t *const sK = lds.k, *const sV = lds.v;
   int wi_block, wi_head;
-  work_item(p.n_blocks, p.H, wi_block, wi_head);
-  const int32_t* blk = p.dtab + p.list_off + (p.block0 + wi_block) * DA_WORDS;
+  work_item(p.n_blocks, p.H, wi_block, wi_head, id);
+  const int32_t* blk = p.dtab + list_off + (p.block0 + wi_block) * DA_WORDS;
   const int first = blk[DA_FIRST_ROW], len = blk[DA_LEN], q0 = blk[DA_BLOCK0];
   const int hc = wi_head * D;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, li = lane & 31, half = lane >> 5;
@@ -594,7 +583,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_bwd_q(AttnParams p) {
 // window.  So the queries from sink_far on are cut into spans of SINK_SPAN: sink_parts workgroups a span, 32 keys and a key/value
 // head, at the head of the same launch, its waves take 32 queries at a time each (no barrier in the loop, tiles of their own in LDS),
 // their sums are added in LDS in a fixed order and the fp32 rows go to the workspace, as do the first block's own of these keys;
-// join_sinks adds them in order, beside dQ.  (In a launch of their own, the first block's workgroup adding what they left: window 1024, 4 first
+// join_sinks adds them in order.  (In a launch of their own, the first block's workgroup adding what they left: window 1024, 4 first
 // keys, 17637 tokens, 40 heads of 128, backward 1512 us, 1515 now; 16384 + 9001 tokens, 16 / 4 heads, window 2048, 1826, 1592; 2048 tokens, 32 / 4
 // heads 246, 170; 500 tokens, 4 / 1 heads, window 64, 68, 32.)
 constexpr int SINK_SPAN = kAttnSinkSpan * BLK, SINK_TILE = 32;
@@ -734,17 +723,19 @@ __device__ __forceinline__ void walk_sinks(const AttnParams& p, SinkLds<D>& lds)
     for (int dt = 0; dt < DT; ++dt) put_sums<D>(out, p.n_sinks, dt, dk[dt], dv[dt]);
   }
 }
-// Every part's rows of a sequence's first keys added in their order: near ones, far ones (256 threads)
+// Every part's rows of a sequence's first keys added in their order: near ones, far ones.  256 pieces of 16 bytes a workgroup.
+__host__ __device__ __forceinline__ int sink_joins(int n_sinks, int D) { return (n_sinks * (D / 2) + 255) / 256; }
 template <int D>
-__device__ void join_sinks(const AttnParams& p, int id) {
-  const int head = id % p.Hkv;
-  const int32_t* blk = p.dtab + p.dtab[DH_ATT_OFF_SPANS] + id / p.Hkv * DA_WORDS;
+__device__ __forceinline__ void join_sinks(const AttnParams& p, int id) {
+  const int n = sink_joins(p.n_sinks, D), piece = id % n, head = id / n % p.Hkv;
+  const int32_t* blk = p.dtab + p.dtab[DH_ATT_OFF_SPANS] + id / n / p.Hkv * DA_WORDS;
   const int first = blk[DA_FIRST_ROW], len = blk[DA_LEN], far = sink_far(p, len);
   if (blk[DA_BLOCK0] != 0 || far >= len) return;             // (a sequence once; without far queries the first block has stored its rows)
   const int slot = blk[DA_SINK_SLOT], rows = p.n_sinks * (D / 4);
   const int n0 = far / SINK_SPAN * p.sink_parts, n1 = (len + SINK_SPAN - 1) / SINK_SPAN * p.sink_parts;
   const size_t step = (size_t)p.Hkv * p.n_sinks * (2 * D);
-  for (int e = threadIdx.x; e < 2 * rows; e += 256) {
+  const int e = 256 * piece + (int)threadIdx.x;
+  if (e < 2 * rows) {
     float4 s{0.f, 0.f, 0.f, 0.f};
     auto add = [&](const float* q) {
       const float4 a = *(const float4*)q;
@@ -793,7 +784,7 @@ __device__ __forceinline__ void store_kv(const AttnParams& p, int row, int hc, i
 }
 // The parts of a key block's walk added in their order, 32 columns of a head (256 threads)
 template <int D>
-__device__ void join_parts(const AttnParams& p, int id) {
+__device__ __forceinline__ void join_parts(const AttnParams& p, int id) {
   const int dt = id % Dim<D>::DT, head = id / Dim<D>::DT % p.Hkv, block = id / Dim<D>::DT / p.Hkv;
   const int32_t* blk = p.dtab + p.dtab[DH_ATT_OFF_BWD] + block * DA_WORDS;
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, kl = blk[DA_BLOCK0] + 32 * (tid >> 6) + (lane & 31);
@@ -811,35 +802,24 @@ __device__ void join_parts(const AttnParams& p, int id) {
   if (kl < blk[DA_LEN] && !joined_later(p, kl, blk[DA_LEN])) store_kv<D>(p, blk[DA_FIRST_ROW] + kl, head * D, half, dt, dk, dv);
 }
 
-// WIN: a key block walks the queries up to its last key's window; what the first keys get from those beyond comes from walk_sinks, for
-// which the launch's first workgroups are.
+// WIN: a key block walks the queries up to its last key's window; what the first keys get from those beyond comes from walk_sinks.
 // Where the blocks are few, a walk (over the queries of every head of the group) is cut into kv_parts runs of steps, a workgroup
-// each, whose fp32 sums join_parts adds beside dQ.
+// each, whose fp32 sums join_parts adds.
+constexpr int QT = 32;                         // queries staged per step
+template <int D>
+struct KvLds {
+  bf16_t q[QT * Dim<D>::TP], d[QT * Dim<D>::TP];
+  bf16_t v[BLK * Dim<D>::KP];                    // the block's own V rows (B operand of dO V^T), kept here to save registers
+  float lse[QT], delta[QT];
+};
 template <int D, bool WIN>
-__global__ __launch_bounds__(256, 2) void k_attn_bwd_kv(AttnParams p) {
+__device__ __forceinline__ void walk_queries(const AttnParams& p, KvLds<D>& lds, unsigned id) {
   constexpr int KS = Dim<D>::KS, DT = Dim<D>::DT, DP = Dim<D>::DP, KP = Dim<D>::KP, TP = Dim<D>::TP;
-  constexpr int QT = 32;                       // queries staged per step
-  struct Lds {
-    bf16_t q[QT * TP], d[QT * TP];
-    bf16_t v[BLK * KP];                          // the block's own V rows (B operand of dO V^T), kept here to save registers
-    float lse[QT], delta[QT];
-  };
-  __shared__ __align__(16) char lds_bytes[WIN && sizeof(SinkLds<D>) > sizeof(Lds) ? sizeof(SinkLds<D>) : sizeof(Lds)];
-  Lds& lds = *(Lds*)lds_bytes;
   bf16_t *const sQ = lds.q, *const sD = lds.d, *const sVf = lds.v;
   float *const sLse = lds.lse, *const sDelta = lds.delta;
   int wi_block, wi_head, part = 0;             // wi_head: a key/value head
-  if constexpr (WIN) {
-    if (blockIdx.x < p.sink_wgs) {
-      walk_sinks<D>(p, *(SinkLds<D>*)lds_bytes);
-      return;
-    }
-    work_item(p.n_blocks, p.Hkv * p.kv_parts, wi_block, wi_head, blockIdx.x - p.sink_wgs);
-    part = wi_head % p.kv_parts;
-    wi_head /= p.kv_parts;
-  } else {
-    work_item(p.n_blocks, p.Hkv, wi_block, wi_head);
-  }
+  work_item(p.n_blocks, WIN ? p.Hkv * p.kv_parts : p.Hkv, wi_block, wi_head, id);
+  if constexpr (WIN) { part = wi_head % p.kv_parts; wi_head /= p.kv_parts; }
   const int32_t* blk = p.dtab + p.list_off + (p.block0 + wi_block) * DA_WORDS;
   const int first = blk[DA_FIRST_ROW], len = blk[DA_LEN], k0 = blk[DA_BLOCK0];
   const int hc = wi_head * D;
@@ -981,6 +961,45 @@ __global__ __launch_bounds__(256, 2) void k_attn_bwd_kv(AttnParams p) {
   if (kok && !later)
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) store_kv<D>(p, first + kl, hc, half, dt, dk[dt], dv[dt]);
+}
+
+template <int D>
+__global__ __launch_bounds__(256, 2) void k_attn_bwd_q(AttnParams p) {
+  __shared__ __align__(16) char lds[sizeof(QLds<D>)];
+  walk_keys<D, false>(p, *(QLds<D>*)lds, blockIdx.x, p.list_off);
+}
+template <int D>
+__global__ __launch_bounds__(256, 2) void k_attn_bwd_kv(AttnParams p) {
+  __shared__ __align__(16) char lds[sizeof(KvLds<D>)];
+  walk_queries<D, false>(p, *(KvLds<D>*)lds, blockIdx.x);
+}
+// Through a window: dK, dV, dQ and the padding rows in one launch, so that the one fills the other's end.  (17637 tokens, window 1024, 40 heads of
+// 128, backward 1508 us in two launches, 1495 in one; 16384 + 9001, window 2048, 16 / 4 heads 1594, 1558; 3172 in eight sequences, window 256, 32 heads
+// 117, 96; 1024, window 256, 8 heads 50, 39; heads of 64, whose dQ alone leaves registers for a third workgroup: 80 of them, 17637 tokens 1600, 1643, but 16 / 4
+// of them, 12000 tokens, 312, 262.)
+template <int D>
+__global__ __launch_bounds__(256, 2) void k_attn_bwd_win(AttnParams p) {
+  __shared__ __align__(16) char lds[std::max({sizeof(KvLds<D>), sizeof(SinkLds<D>), sizeof(QLds<D>)})];
+  const unsigned id = blockIdx.x;
+  if (id < p.sink_wgs) {
+    walk_sinks<D>(p, *(SinkLds<D>*)lds);
+  } else if (id < p.q_from) {
+    if (id - p.sink_wgs < p.kv_wgs) walk_queries<D, true>(p, *(KvLds<D>*)lds, id - p.sink_wgs);
+  } else if (id < p.zero_from) {
+    walk_keys<D, true>(p, *(QLds<D>*)lds, id - p.q_from, p.dtab[DH_ATT_OFF_FWD]);
+  } else {
+    const int item = (int)(id - p.zero_from);
+    clear_padding(p, item, p.dQ, p.ldq, p.H * D);
+    clear_padding(p, item, p.dK, p.ldk, p.Hkv * D);
+    clear_padding(p, item, p.dV, p.ldv, p.Hkv * D);
+  }
+}
+// What its workgroups left to be added
+template <int D>
+__global__ __launch_bounds__(256) void k_attn_join_kv(AttnParams p) {
+  const int joins = p.kv_parts > 1 ? p.n_blocks * p.Hkv * Dim<D>::DT : 0, id = (int)blockIdx.x;
+  if (id < joins) join_parts<D>(p, id);
+  else join_sinks<D>(p, id - joins);
 }
 
 // ------------------------------------------------------------------------------------------------ short sequences
@@ -1384,9 +1403,12 @@ mux_status check_window(const char* fn, int32_t window, int32_t n_sinks) {
   if (n_sinks > MUX_ATTN_MAX_SINKS) return fail(MUX_ERR_UNSUPPORTED, std::string(fn) + ": n_sinks above MUX_ATTN_MAX_SINKS");
   return MUX_OK;
 }
-// (the WIN kernels' lanes reach the rows of a tile with 32 bits)
-mux_status check_rows(const char* fn, const mux_attn_desc* d, Window w) {
+// (the WIN kernels' lanes reach the rows of a tile with 32 bits; a launch is held to 2^32 threads)
+mux_status check_rows(const char* fn, const mux_attn_desc* d, const mux_segtab* st, Window w) {
   const int64_t most = (int64_t)1 << 24;
+  const int64_t wgs = st->n_attn_blocks * ((int64_t)d->n_heads + d->n_kv_heads) + st->n_attn_spans * (int64_t)d->n_kv_heads * 2 + (int64_t)st->items[0].size();
+  if (w.window > 0 && wgs >= most - 32 * kComputeUnits)        // (workgroups that share a walk are counted where they are few)
+    return fail(MUX_ERR_SHAPE, std::string(fn) + ": too many work items");
   if (w.window > 0 && (d->ldq >= most || d->ldk >= most || d->ldv >= most || d->ldo >= most))
     return fail(MUX_ERR_SHAPE, std::string(fn) + ": a leading dimension of 2^24 elements or more");
   return MUX_OK;
@@ -1399,7 +1421,7 @@ Window effective(const mux_segtab* st, int32_t window, int32_t n_sinks) {
 mux_status forward(const char* fn, const mux_attn_desc* desc, Window w, const mux_segtab* st, const void* dev_segtab, const void* Q,
                    const void* K, const void* V, void* O, void* saved, void* hip_stream) {
   if (mux_status s = check(fn, desc, st)) return s;
-  if (mux_status s = check_rows(fn, desc, w)) return s;
+  if (mux_status s = check_rows(fn, desc, st, w)) return s;
   if (st->T == 0) return MUX_OK;
   if (!dev_segtab || !Q || !K || !V || !O) return fail(MUX_ERR_INVALID_ARG, std::string(fn) + ": null device pointer");
   if (!aligned16(Q) || !aligned16(K) || !aligned16(V) || !aligned16(O))
@@ -1438,7 +1460,7 @@ mux_status forward(const char* fn, const mux_attn_desc* desc, Window w, const mu
 // Workgroups that share a key block's walk.  Places are two a compute unit; with fewer workgroups than places the launch takes the
 // longest walk, with more their total and about half a walk until the last is done.  Beside that, in steps of 32 queries (1.4 to 2.3
 // us): the parts' sums, 128 KB each at 128 columns, 1 to 5 while all have a place and are read back from the caches, some 20 more for every chip
-// full after that; and a part walks three steps at least.  Window 1024, heads of 128, backward, walk in one part -> in n: 2048 tokens, 8 heads a
+// full after that (at most eight, 512 MB); and a part walks three steps at least.  Window 1024, heads of 128, backward, walk in one part -> in n: 2048 tokens, 8 heads a
 // key/value head and 4 of those (64 workgroups), 8 parts 700 -> 259 us; 4096 tokens, 4 and 8 (256), 2 parts 471 -> 373, 3 parts 416; window 300, 3000 tokens, 4
 // and 6 (144), 3 parts 177 -> 126, 4 parts 139; window 2048, 16384 + 9001 tokens, 4 and 4 (796), 2 parts 1985 -> 1787, 3 parts 1879; window 512, 9600
 // tokens, 4 and 8 (600), 2 parts 617 -> 616, 3 parts 625.
@@ -1450,6 +1472,7 @@ int kv_parts(const mux_segtab* st, const mux_attn_desc* desc, Window w, int n_lo
   double least = 0;
   for (int n = 1; n <= 16 && (n == 1 || 3 * n <= walk); ++n) {
     const double full = wgs * n / (2 * kComputeUnits);
+    if (n > 1 && full > 8) break;
     const double cost = (full <= 1 ? walk / n : full * walk / n + walk / (2 * n)) + (n == 1 ? 0 : full <= 1 ? 1 + 4 * full : 5 + 20 * (full - 1));
     if (n == 1 || cost < least) { best = n; least = cost; }
   }
@@ -1485,7 +1508,7 @@ mux_status backward(const char* fn, const mux_attn_desc* desc, Window w, const m
                     const void* K, const void* V, const void* O, const void* dO, const void* saved, void* dQ, void* dK, void* dV,
                     void* ws, size_t ws_bytes, void* hip_stream) {
   if (mux_status s = check(fn, desc, st)) return s;
-  if (mux_status s = check_rows(fn, desc, w)) return s;
+  if (mux_status s = check_rows(fn, desc, st, w)) return s;
   if (st->T == 0) return MUX_OK;
   if (!dev_segtab || !Q || !K || !V || !O || !dO || !saved || !dQ || !dK || !dV || !ws)
     return fail(MUX_ERR_INVALID_ARG, std::string(fn) + ": null device pointer");
@@ -1519,22 +1542,27 @@ mux_status backward(const char* fn, const mux_attn_desc* desc, Window w, const m
     const size_t n = (size_t)st->T * desc->n_heads;
     p.n_blocks = n_long;
     ATTN_LAUNCH("attn_delta", k_attn_delta, D, dim3((unsigned)(((n + 3) / 4 * 16 + 255) / 256)), stream, p);
-    p.n_long = n_long;
-    p.kv_parts = plan.parts; p.sink_parts = plan.sink_parts;
-    p.n_spans = st->n_attn_spans;
-    p.sink_wgs = plan.sink_wgs;
-    if (plan.parts > 1) p.parts = (float*)((char*)ws + plan.part);
-    if (plan.sink_wgs > 0) { p.near = (float*)((char*)ws + plan.near); p.far = (float*)((char*)ws + plan.far); }
-    const unsigned kv_items = (unsigned)n_long * (unsigned)desc->n_kv_heads;
-    ATTN_LAUNCH_WIN("attn_bwd_kv", k_attn_bwd_kv, D, win, dim3(p.sink_wgs + kv_items * (unsigned)p.kv_parts), stream, p);
+    const unsigned kv_items = (unsigned)n_long * (unsigned)desc->n_kv_heads, q_items = (unsigned)n_long * (unsigned)desc->n_heads;
     AttnParams q = p;
     q.list_off = st->dev_image[DH_ATT_OFF_FWD];
-    q.zero_from = (unsigned)n_long * (unsigned)desc->n_heads;
-    unsigned wgs = q.zero_from;
-    if (p.kv_parts > 1) wgs += kv_items * (unsigned)((D + 31) / 32);
-    if (p.far) wgs += (unsigned)p.n_spans * (unsigned)desc->n_kv_heads;
-    if (pads && ride) wgs += (unsigned)st->items[0].size();
-    ATTN_LAUNCH_WIN("attn_bwd_q", k_attn_bwd_q, D, win, dim3(wgs), stream, q);
+    if (!win) {
+      ATTN_LAUNCH("attn_bwd_kv", k_attn_bwd_kv, D, dim3(kv_items), stream, p);
+      ATTN_LAUNCH("attn_bwd_q", k_attn_bwd_q, D, dim3(q_items), stream, q);
+    } else {
+      q = p;
+      q.kv_parts = plan.parts; q.sink_parts = plan.sink_parts;
+      q.n_spans = st->n_attn_spans;
+      q.sink_wgs = plan.sink_wgs;
+      q.kv_wgs = kv_items * (unsigned)plan.parts;
+      if (plan.parts > 1) q.parts = (float*)((char*)ws + plan.part);
+      if (plan.sink_wgs > 0) { q.near = (float*)((char*)ws + plan.near); q.far = (float*)((char*)ws + plan.far); }
+      q.q_from = q.sink_wgs + (q.kv_wgs + 7) / 8 * 8;
+      q.zero_from = q.q_from + q_items;
+      ATTN_LAUNCH("attn_bwd_win", k_attn_bwd_win, D, dim3(q.zero_from + (pads ? (unsigned)st->items[0].size() : 0u)), stream, q);
+      const unsigned joins = (plan.parts > 1 ? kv_items * (unsigned)((D + 31) / 32) : 0u) +
+                             (q.far ? (unsigned)q.n_spans * (unsigned)desc->n_kv_heads * (unsigned)sink_joins(w.n_sinks, D) : 0u);
+      if (joins > 0) ATTN_LAUNCH("attn_join_kv", k_attn_join_kv, D, dim3(joins), stream, q);
+    }
   }
   if (n128 + n64 > 0) {
     p.block0 = n_long;

@@ -139,6 +139,13 @@ def test_heads(env, d, H, G):
     Call(env, [[64] * 5, [128] * 3, [100]], 64, H, 20, 2, seed=d + H + 1, G=G, d=d).both().check()
 
 
+@pytest.mark.parametrize("lens,H,G,d,window,sinks", [([[700], [650, 300]], 48, 48, 64, 90, 5), ([[2000]], 16, 1, 64, 1000, 4),
+                                                     ([[1, 900, 3], [770]], 10, 2, 80, 333, 64), ([[1100], [300]], 5, 5, 128, 500, 0)])
+def test_key_blocks_many_and_few(env, lens, H, G, d, window, sinks):
+    """A workgroup a key block; sixteen that share one's walk over a large group; runs that end inside a head and a ragged last block."""
+    Call(env, lens, 64, H, window, sinks, seed=window + H, G=G, d=d).both().check()
+
+
 @pytest.mark.parametrize("chunk,pack,flags", [(1, 0, 0), (16, 500, 0), (64, 0, 1)])
 def test_tables(env, chunk, pack, flags):
     Call(env, [[140, 700], [3], [90, 333]], chunk, 2, 77, 9, seed=3, pack=pack, flags=flags, d=64).both().check()

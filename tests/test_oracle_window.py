@@ -71,4 +71,28 @@ def test_refusals(mx):
     desc = mx.AttnDesc(2, 64, W, W, W, W)
     base = mx.mux_attn_workspace_bytes(desc, st)
     size = lambda w, z: mx.mux_attn_window_workspace_bytes(desc, w, z, st)                       # noqa: E731
-    assert size(300, 4) == size(40, 0) == size(200, 64) == base < size(40, 4) < size(40, 64) and size(0, 4) == 0 and size(4, 65) == 0
+    assert size(300, 4) == base <= size(40, 0) <= size(200, 64) and size(40, 0) < size(40, 4) < size(40, 64) and size(0, 4) == 0 and size(4, 65) == 0
+
+
+def test_launches_that_would_not_fit(mx):
+    """A launch is held to 2^32 threads: what would take more is refused before anything runs."""
+    M = 1 << 40
+    st = mx.mux_segtab_build([mx.TaskDesc(0, 0, 1.0, [1] * 65536 + [300])], 256)
+    desc = lambda h, kv: mx.AttnDesc(h, 64, h * 64, kv * 64, kv * 64, h * 64, 0.0, kv)                               # noqa: E731
+    for h, kv in ((256, 1), (128, 128)):
+        with pytest.raises(mx.MuxError) as e:
+            mx.mux_attn_window_forward(desc(h, kv), 40, 4, st, M, 2 * M, 3 * M, 4 * M, 5 * M, 6 * M)
+        assert e.value.status == 2 and "too many" in str(e.value)
+        with pytest.raises(mx.MuxError) as e:
+            mx.mux_attn_window_backward(desc(h, kv), 40, 4, st, M, 2 * M, 3 * M, 4 * M, 5 * M, 6 * M, 7 * M, 8 * M, 9 * M, 10 * M, 11 * M, M)
+        assert e.value.status == 2 and "too many" in str(e.value)
+
+
+def test_workspace_where_keys_are_few(mx):
+    """The partial sums of dK, dV are bounded, however long the walk."""
+    for lens, h, kv, w, z in (([2048], 32, 4, 1024, 4), ([16384, 9001], 16, 4, 2048, 16), ([1 << 20], 64, 1, 1 << 19, 64), ([64, 300], 4, 1, 64, 0)):
+        st = mx.mux_segtab_build([mx.TaskDesc(0, 0, 1.0, lens)], 256)
+        desc = mx.AttnDesc(h, 128, h * 128, kv * 128, kv * 128, h * 128, 0.0, kv)
+        size, base = mx.mux_attn_window_workspace_bytes(desc, w, z, st), mx.mux_attn_workspace_bytes(desc, st)
+        sinks = 2 * sum(-(-n // 512) for n in lens) * kv * z * 128 * 4 * (16 + 256)
+        assert base < size <= base + (4096 << 17) + sinks + 1024
