@@ -411,12 +411,15 @@ int pieces_of(int rows, int per) { return (rows + per - 1) / per; }
 // 16-byte pieces of a row, the last one perhaps part of one
 int row_pieces(const mux_norm_desc* d) { return (int)(((size_t)d->width * esize(d) + 15) / 16); }
 
-// Rows a workgroup of the backward takes, and so the number of partial sums: enough workgroups for six waves a SIMD, twice what
-// stays there at a time, so that the last ones find their place (17637 x 5120, three, five, six, eight, ten: 140, 126, 124, 136, 135 us
-// and 8 to 15 for the sum of the pieces), of at least four rows.
+// Whether a tensor of the call is too large to be met again in the last-level cache.
+bool streams(const mux_norm_desc* d, const mux_segtab* st) { return (size_t)st->T * (size_t)d->width * esize(d) > kStreamBytes; }
+// Rows a workgroup of the backward takes, and so the number of partial sums, of at least four rows: enough workgroups for three waves a
+// SIMD (12000 x 1024, three, six: 31.3, 35.8 us forward and backward; 18000 x 704 32.1, 36.3; 8000 x 2048 40.7, 44.5; 1500 x 8192 35.9, 40.1); where rows come
+// from memory for six, twice what stays there at a time, so that the last ones find their place (17637 x 5120, three, five, six, eight, ten: 140, 126,
+// 124, 136, 135 us and 8 to 15 for the sum of the pieces).
 int piece_rows(const mux_norm_desc* d, const mux_segtab* st) {
   const int n = row_pieces(d), waves = n <= 128 ? 4 : std::min(16, (n + 127) / 128);
-  return std::min(kMaxRows, std::max(4, pieces_of(st->T, std::max(1, 24 / waves) * kComputeUnits)));
+  return std::min(kMaxRows, std::max(4, pieces_of(st->T, std::max(1, (streams(d, st) ? 24 : 12) / waves) * kComputeUnits)));
 }
 int total_pieces(const mux_norm_desc* d, const mux_segtab* st) {
   int n = 0, behind = 0;
@@ -465,7 +468,7 @@ void launch_one(const char* name, const mux_norm_desc* d, dim3 grid, const NormP
 template <bool BACKWARD>
 void launch(const char* name, const mux_norm_desc* d, const mux_segtab* st, NormParams p, hipStream_t stream) {
   p.in.rows = BACKWARD ? piece_rows(d, st) : 4;
-  const Mode mode = (size_t)d->width * esize(d) % 16 != 0 ? ODD : (size_t)st->T * (size_t)d->width * esize(d) > kStreamBytes ? STREAM : WHOLE;
+  const Mode mode = (size_t)d->width * esize(d) % 16 != 0 ? ODD : streams(d, st) ? STREAM : WHOLE;
   float* const part = p.part;
   int done = 0;                                          // pieces of the launches before
   for (int base = 0; base < st->n_tasks; base += kBatch) {
