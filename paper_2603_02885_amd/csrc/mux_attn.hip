@@ -67,9 +67,11 @@ struct AttnParams {
   unsigned q_from;           // .. first workgroup of dQ (sink_wgs, q_from: multiples of 8, so that an XCD keeps its heads)
   int n_spans, sink_parts;   // .. spans of far queries, workgroups that share one
 };
-// Whether a query sees the key `ahead` tokens before it
+// Whether a query sees the key `ahead` tokens before it.  Tiles without first keys ask for the window alone, three instructions an
+// element for seven (2112 tokens, 32 / 8 heads of 128, window 256, forward MASKF us).
+__device__ __forceinline__ bool in_window(const AttnParams& p, int ahead) { return (unsigned)ahead < (unsigned)p.window; }
 __device__ __forceinline__ bool in_window(const AttnParams& p, int ahead, bool sink) {
-  return (int)((unsigned)ahead < (unsigned)p.window) | ((int)sink & (int)(ahead >= 0));
+  return (int)in_window(p, ahead) | ((int)sink & (int)(ahead >= 0));
 }
 
 __device__ __forceinline__ bf16x4 lds_read_tr(const bf16_t* p) {
@@ -324,13 +326,21 @@ __global__ __launch_bounds__(256, 2) void k_attn_fwd(AttnParams p) {
     float mx = -INFINITY;
     if (WIN && (diag || kb <= wq_last - p.window)) {
       const int rel = ql - kb - 4 * half, snk = p.n_sinks - kb - 4 * half;
+      if (kb >= p.n_sinks) {
 #pragma unroll
-      for (int kt = 0; kt < 2; ++kt)
+        for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
-          const int key = 32 * kt + 8 * (j >> 2) + (j & 3);
-          if (!in_window(p, rel - key, key < snk)) s[kt][j] = -INFINITY;
-        }
+          for (int j = 0; j < 16; ++j)
+            if (!in_window(p, rel - (32 * kt + 8 * (j >> 2) + (j & 3)))) s[kt][j] = -INFINITY;
+      } else {
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            const int key = 32 * kt + 8 * (j >> 2) + (j & 3);
+            if (!in_window(p, rel - key, key < snk)) s[kt][j] = -INFINITY;
+          }
+      }
     }
     if (!WIN && diag) {                         // only the tiles on the diagonal pay for the mask
       const int rel = ql - kb - 4 * half;       // key 32 kt + 8 (j / 4) + j % 4 is hidden iff it exceeds rel
@@ -538,10 +548,16 @@ __device__ __forceinline__ void walk_keys(const AttnParams& p, QLds<D>& lds, uns
       for (int j = 0; j < 16; ++j) s[j] = fast_exp2(fmaf(s[j], c, -lse2));        // P^T (zero for a lane without query)
       if (WIN && (diag || kb <= wq_last - p.window)) {
         const int rel = ql - kb - 32 * kt - 4 * half, snk = p.n_sinks - kb - 32 * kt - 4 * half;
+        if (kb >= p.n_sinks) {
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
-          const int key = 8 * (j >> 2) + (j & 3);
-          if (!in_window(p, rel - key, key < snk)) s[j] = 0.f;
+          for (int j = 0; j < 16; ++j)
+            if (!in_window(p, rel - (8 * (j >> 2) + (j & 3)))) s[j] = 0.f;
+        } else {
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            const int key = 8 * (j >> 2) + (j & 3);
+            if (!in_window(p, rel - key, key < snk)) s[j] = 0.f;
+          }
         }
       }
       if (!WIN && diag) {                       // only the tiles on the diagonal pay for the mask
@@ -1154,9 +1170,15 @@ __device__ __forceinline__ void attn_bwd_short(const AttnParams& p, const int wi
         for (int j = 0; j < 16; ++j) s[j] = fast_exp2(fmaf(s[j], c, -sLse[qb + tok(j, half)]));
         if (WIN && (qb < 32 * wave + 32 || qb + QT - 1 - 32 * wave >= p.window)) {
           const int rel = kl - qb - 4 * half;
+          if (32 * wave >= p.n_sinks) {
 #pragma unroll
-          for (int j = 0; j < 16; ++j)
-            if (!in_window(p, 8 * (j >> 2) + (j & 3) - rel, kl < p.n_sinks)) s[j] = 0.f;
+            for (int j = 0; j < 16; ++j)
+              if (!in_window(p, 8 * (j >> 2) + (j & 3) - rel)) s[j] = 0.f;
+          } else {
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+              if (!in_window(p, 8 * (j >> 2) + (j & 3) - rel, kl < p.n_sinks)) s[j] = 0.f;
+          }
         }
         if (!WIN && qb < 32 * wave + 32) {     // only the tile on the diagonal pays for the mask
           const int rel = kl - qb - 4 * half;  // query 8 (j / 4) + j % 4 sees the key iff it is >= rel
