@@ -68,7 +68,7 @@ struct AttnParams {
   int n_spans, sink_parts;   // .. spans of far queries, workgroups that share one
 };
 // Whether a query sees the key `ahead` tokens before it.  Tiles without first keys ask for the window alone, three instructions an
-// element for seven (2112 tokens, 32 / 8 heads of 128, window 256, forward MASKF us).
+// element for seven (2112 tokens, 32 / 8 heads of 128, window 256, forward 27.9 -> 26.5 us).
 __device__ __forceinline__ bool in_window(const AttnParams& p, int ahead) { return (unsigned)ahead < (unsigned)p.window; }
 __device__ __forceinline__ bool in_window(const AttnParams& p, int ahead, bool sink) {
   return (int)in_window(p, ahead) | ((int)sink & (int)(ahead >= 0));
@@ -242,7 +242,7 @@ __device__ __forceinline__ int window_tile(const AttnParams& p, int q0) { return
 
 // ------------------------------------------------------------------------------------------------ forward
 // WIN: the query block walks the tile of the first keys (where some are always visible) and then those of its window.  17637 tokens, 40
-// heads of 128, window 1024, 4 first tokens: 471 us, 604 TFLOP/s of the visible pairs; what is left waits for LDS as without a window.
+// heads of 128, window 1024, 4 first tokens: 463 us, 615 TFLOP/s of the visible pairs; what is left waits for LDS as without a window.
 template <int D, bool WIN>
 __global__ __launch_bounds__(256, 2) void k_attn_fwd(AttnParams p) {
   constexpr int KS = Dim<D>::KS, DT = Dim<D>::DT, DP = Dim<D>::DP, KP = Dim<D>::KP, TP = Dim<D>::TP;
@@ -534,6 +534,8 @@ __device__ __forceinline__ void walk_keys(const AttnParams& p, QLds<D>& lds, uns
     const bool diag = kb + TILE - 1 > wq_first;
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt) {            // one half of the tile at a time keeps the live registers down
+      // (a half that none of the wave's queries sees; the forward left it out too: heads of 64 8 % slower for the registers, others +-3 %)
+      if (WIN && (kb + 32 * kt > wq_last || (kb + 32 * kt + 31 <= wq_first - p.window && kb + 32 * kt >= p.n_sinks))) continue;
       f32x16 s, dp;
 #pragma unroll
       for (int j = 0; j < 16; ++j) { s[j] = 0.f; dp[j] = 0.f; }
