@@ -1481,24 +1481,22 @@ mux_status forward(const char* fn, const mux_attn_desc* desc, Window w, const mu
   return last_hip(fn);
 }
 
-// Workgroups that share a key block's walk.  Places are two a compute unit; with fewer workgroups than places the launch takes the
-// longest walk, with more their total and about half a walk until the last is done.  Beside that, in steps of 32 queries (1.4 to 2.3
-// us): the parts' sums, 128 KB each at 128 columns, 1 to 5 while all have a place and are read back from the caches, some 20 more for every chip
-// full after that (at most eight, 512 MB); and a part walks three steps at least.  Window 1024, heads of 128, backward, walk in one part -> in n: 2048 tokens, 8 heads a
-// key/value head and 4 of those (64 workgroups), 8 parts 700 -> 259 us; 4096 tokens, 4 and 8 (256), 2 parts 471 -> 373, 3 parts 416; window 300, 3000 tokens, 4
-// and 6 (144), 3 parts 177 -> 126, 4 parts 139; window 2048, 16384 + 9001 tokens, 4 and 4 (796), 2 parts 1985 -> 1787, 3 parts 1879; window 512, 9600
-// tokens, 4 and 8 (600), 2 parts 617 -> 616, 3 parts 625.
+// Workgroups that share a key block's walk.  The launch, dQ with it (three quarters of the steps), takes its total over the chip's places, two a
+// compute unit, or the longest walk if that is more.  A cut walk costs the parts' sums, 128 KB each at 128 columns, in steps of 32 queries (1.4 to 2.3 us)
+// about one and one more for 32 workgroups; a part walks four steps at least.  Backward with the walk in 1, 2, 3, 4, 6 parts (chosen: *), us: 2048 tokens, 4 groups of 8
+// heads of 128, window 1024 (64 workgroups) 549, 276, 214, 166, 153 (5*); 4096, 8 of 4, the same (256) 330, 298*, 313, 312, 346; 3000, 6 of 4, window 300
+// (144) 113, 91*, 96, 95, 105; 500, one of 4, window 64 (4) 58, 36, 30, 26, 25*; 1024, 8 heads, window 256 (64) 35, 31*, 35, 37, 40; 2000, 8 heads, window 128 (128) 33*, 39,
+// 52, 54, 65; 16384 + 9001, 4 of 4, window 2048 (796) 1551*, 1544, 1667, 1617, 1704; 9600, 8 of 4, window 512 (600) 430*, 496, 538, 582, 621.
 int kv_parts(const mux_segtab* st, const mux_attn_desc* desc, Window w, int n_long) {
   if (w.window == 0 || n_long == 0) return 1;
   const double wgs = (double)n_long * desc->n_kv_heads, group = desc->n_heads / desc->n_kv_heads;
   const double walk = group * (double)((std::min<int64_t>(st->attn_longest, (int64_t)w.window + kAttnBlockRows - 1) + 31) / 32);
+  const double total = 1.75 * wgs * walk / (2 * kComputeUnits);
   int best = 1;
-  double least = 0;
-  for (int n = 1; n <= 16 && (n == 1 || 3 * n <= walk); ++n) {
-    const double full = wgs * n / (2 * kComputeUnits);
-    if (n > 1 && full > 8) break;
-    const double cost = (full <= 1 ? walk / n : full * walk / n + walk / (2 * n)) + (n == 1 ? 0 : full <= 1 ? 1 + 4 * full : 5 + 20 * (full - 1));
-    if (n == 1 || cost < least) { best = n; least = cost; }
+  double least = std::max(walk, total);
+  for (int n = 2; n <= 16 && 4 * n <= walk; ++n) {
+    const double cost = std::max(walk / n, total) + 1 + wgs * n / 32;
+    if (cost < least) { best = n; least = cost; }
   }
   return best;
 }

@@ -95,4 +95,4 @@ def test_workspace_where_keys_are_few(mx):
         desc = mx.AttnDesc(h, 128, h * 128, kv * 128, kv * 128, h * 128, 0.0, kv)
         size, base = mx.mux_attn_window_workspace_bytes(desc, w, z, st), mx.mux_attn_workspace_bytes(desc, st)
         sinks = 2 * sum(-(-n // 512) for n in lens) * kv * z * 128 * 4 * (16 + 256)
-        assert base < size <= base + (4096 << 17) + sinks + 1024
+        assert base < size <= base + (1024 << 17) + sinks + 1024
