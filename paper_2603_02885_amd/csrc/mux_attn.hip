@@ -11,7 +11,9 @@
 // The operand that has to be read across rows (V^T, K^T, dO^T, Q^T) comes from a row-major LDS tile through
 // ds_read_b64_tr_b16.  A sum over 16 tokens may take them in any order as long as both operands agree; the order
 // used is the one the accumulator layout gives: slot i of half-wave h <-> token 8 (i / 4) + 4 h + i % 4.
-// Every output element has one owner; nothing is accumulated across workgroups, results repeat bit for bit.
+// Every output element has one owner; what several workgroups form of one (through a window: dK, dV of long walks) they leave as fp32
+// sums that its owner adds in a fixed order: results repeat bit for bit.  P and dS are rounded to bf16 as operands of the next product
+// (half a step, 2^-9 of each term, which a sum of many averages); scores, statistics and all sums stay in fp32.
 #include <algorithm>
 #include <type_traits>
 
@@ -597,7 +599,7 @@ __device__ __forceinline__ void walk_keys(const AttnParams& p, QLds<D>& lds, uns
 
 // ------------------------------------------------------------------------------------------------ dK, dV of the first keys
 // Every query of a sequence sees its first n_sinks keys.  What they get from the queries of the first key block's own walk
-// (k_attn_bwd_kv) is formed there; for the rest that walk would be as long as the sequence, one workgroup's while all others walk a
+// (walk_queries) is formed there; for the rest that walk would be as long as the sequence, one workgroup's while all others walk a
 // window.  So the queries from sink_far on are cut into spans of SINK_SPAN: sink_parts workgroups a span, 32 keys and a key/value
 // head, at the head of the same launch, its waves take 32 queries at a time each (no barrier in the loop, tiles of their own in LDS),
 // their sums are added in LDS in a fixed order and the fp32 rows go to the workspace, as do the first block's own of these keys;
