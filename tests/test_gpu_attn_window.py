@@ -223,3 +223,24 @@ def test_forward_alone(env):
     c.forward(saved=False)
     c.torch.cuda.synchronize()
     assert c.torch.equal(c.o, o)
+
+
+def test_rows_far_apart(env):
+    """Offsets beyond 32 bits (all tensors columns of one buffer of 2^22 a row): the bits of the same rows side by side."""
+    c = Call(env, [[600, 40], [300], [129]], 64, 4, 100, 5, seed=12, G=2, d=80).both()
+    want = [t.clone() for t in c.outputs()]
+    ld, at, far = 1 << 22, 0, []
+    big = c.torch.empty((c.T, ld), dtype=c.torch.bfloat16, device="cuda")
+    assert c.T * ld > 1 << 31
+    for t in (c.q, c.k, c.v, c.do, *c.outputs()):
+        v = big[:, at:at + t.shape[1]]
+        v.copy_(t)
+        far.append(v)
+        at += t.shape[1] + 8
+    c.q, c.k, c.v, c.do, c.o = far[:5]
+    c.grads = far[5:]
+    for t in c.outputs():
+        t.fill_(float("nan"))
+    c.desc = c.mx.AttnDesc(4, 80, ld, ld, ld, ld, 0.0, 2)
+    c.both()
+    assert all(c.torch.equal(a, b) for a, b in zip(want, c.outputs()))

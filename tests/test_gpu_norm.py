@@ -293,3 +293,26 @@ def test_captured(env):
         graph.replay()
         c.torch.cuda.synchronize()
         assert all(c.torch.equal(a, b) for a, b in zip(want, [c.Y, c.dX] + c.dg + c.db)), k
+
+
+def test_rows_far_apart(env):
+    """Offsets beyond 32 bits (rows of 2^22 elements' distance): the bits of the same rows side by side, nothing else written."""
+    c = Case(env, LENS, 64, 513, 0, seed=14, padx=7, pady=7)
+    c.forward()
+    c.backward()
+    want = [t.clone() for t in (c.Y[:, :513], c.dX[:, :513], *c.dg, *c.db)]
+    ld = 1 << 22
+    assert c.T * ld > 1 << 31
+    far = [c.torch.empty((c.T, ld), dtype=c.td, device="cuda") for _ in range(4)]
+    for f, t in zip(far, (c.X, c.dY, c.Y, c.dX)):
+        f[:, :513] = t[:, :513]
+        f[:, 513:600] = 7.0
+    c.X, c.dY, c.Y, c.dX = far
+    c.desc = c.mx.NormDesc(513, 0, c.gamma, c.beta, EPS, ld, ld, n_tasks=c.n)
+    for t in (c.Y, c.dX):
+        t[:, :513] = float("nan")
+    c.forward()
+    c.backward()
+    got = (c.Y[:, :513], c.dX[:, :513], *c.dg, *c.db)
+    assert all(c.torch.equal(a, b) for a, b in zip(want, got))
+    assert all((t[:, 513:600] == 7.0).all() for t in (c.Y, c.dX))

@@ -270,3 +270,24 @@ def test_repeats_streams_and_capture(env):
         graph.replay()
         c.torch.cuda.synchronize()
         assert all(c.torch.equal(a, b) for a, b in zip(want, outs)), k
+
+
+def test_rows_far_apart(env):
+    """Offsets beyond 32 bits (rows of 2^23 elements' distance): the bits of the same rows side by side, nothing else written."""
+    c = Case(env, LENS, 64, 9001, 0, PAIRS, seed=15, pad=7, padg=7)
+    c.forward()
+    c.backward()
+    want = [t.clone() for t in (c.row_logp, c.logp, c.loss, c.dx[:, :9001])]
+    ld = 1 << 23
+    assert c.T * ld > 1 << 31
+    far = [c.torch.empty((c.T, ld), dtype=c.td, device="cuda") for _ in range(2)]
+    far[0][:, :9001] = c.x[:, :9001]
+    far[1][:, :9100] = 7.0
+    c.x, c.dx = far
+    c.desc = c.mx.PrefDesc(9001, 0, ld, ld)
+    for t in (c.row_logp, c.logp, c.loss):
+        t.fill_(float("nan"))
+    c.forward()
+    c.backward()
+    assert all(c.torch.equal(a, b) for a, b in zip(want, (c.row_logp, c.logp, c.loss, c.dx[:, :9001])))
+    assert (c.dx[:, 9001:9100] == 7.0).all()
