@@ -245,8 +245,9 @@ __device__ __forceinline__ int window_tile(const AttnParams& p, int q0) { return
 // ------------------------------------------------------------------------------------------------ forward
 // WIN: the query block walks the tile of the first keys (where some are always visible) and then those of its window.  17637 tokens, 40
 // heads of 128, window 1024, 4 first tokens: 463 us, 615 TFLOP/s of the visible pairs; without global loads 409, nor LDS writes 377, nor
-// exponentials 346: the operands' way out of LDS, 32 KB a wave and tile, as without a window.  (Half tiles where the other half is hidden, V fragments
-// fetched before the softmax, two and three waves a SIMD: no faster, heads of 64 8 to 17 % slower.)
+// exponentials 346 (operand reads, 32 KB a wave and tile, and products), one wave a SIMD 602.  The matrix cores are busy 36 % of 1.8 GHz, LDS 38 %, the
+// vector units 41 %.  Half tiles where the other half is hidden and V fragments fetched before the softmax were no faster, heads of 64 8 to 17 % slower;
+// LDS pitches with fewer bank conflicts +-1 %.
 template <int D, bool WIN>
 __global__ __launch_bounds__(256, 2) void k_attn_fwd(AttnParams p) {
   constexpr int KS = Dim<D>::KS, DT = Dim<D>::DT, DP = Dim<D>::DP, KP = Dim<D>::KP, TP = Dim<D>::TP;
