@@ -582,7 +582,7 @@ def attention(mx, torch, args):
     lens = [n for t in wl.tasks for n in t.seq_lens]
     seen = lambda n: sum(min(i + 1, w) + min(z, max(0, i + 1 - w)) for i in range(n)) if w else n * (n + 1) // 2      # noqa: E731
     pairs = float(sum(seen(n) for n in lens)) * H
-    flops = {"attn_fwd": 4.0 * d * pairs, "attn_bwd_kv": 6.0 * d * pairs, "attn_bwd_q": 4.0 * d * pairs}
+    flops = {"attn_fwd": 4.0 * d * pairs, "attn_bwd_kv": 6.0 * d * pairs, "attn_bwd_q": 4.0 * d * pairs, "attn_bwd_win": 10.0 * d * pairs}
     kernels = {}
     for e in prof:
         k = {"launches": e["launches"], "avg_us": e["total_ms"] * 1e3 / max(e["launches"], 1)}
